@@ -117,7 +117,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2410_13276_amd.build` (no CPU fallback exists)")
         L = C.CDLL(LIB_PATH)
-        for name, (args, res) in _SIGS.items():
+        for name, (args, res) in (*_SIGS.items(), *_DECODE_SIGS.items()):
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = res
@@ -594,3 +594,9 @@ def bsattn_varlen(q, k, v, cu_seqlens, mask: VarlenMask, *, causal: bool = True,
                                   _stream(stream))
     _check(st, "seer_bsattn_varlen")
     return out, lse
+
+
+# generation: rotary positions, the paged cache, and attention over it
+from .decode import SIGS as _DECODE_SIGS  # noqa: E402
+from .decode import (alloc_kv_cache, kv_append, paged_attn, paged_attn_workspace_bytes,  # noqa: E402,F401
+                     rope, rope_freqs, rope_grad)
