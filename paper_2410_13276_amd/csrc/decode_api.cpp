@@ -36,6 +36,14 @@ seer_status check_written(const int64_t (&st)[3], const int32_t (&n)[3], int32_t
   return SEER_OK;
 }
 
+// The attention counts a cache's strides in 16-byte pieces of 32 bits.
+seer_status check_cache_strides(const int64_t (&st)[3], int32_t dtype) {
+  const seer_status s = check_strides(st, dtype);
+  if (s != SEER_OK) return s;
+  const int64_t vec = dtype == SEER_F32 ? 4 : 8;
+  return st[0] / vec <= UINT32_MAX && st[2] / vec <= UINT32_MAX ? SEER_OK : SEER_ERR_UNSUPPORTED;
+}
+
 seer_status check_rope(const seer_rope_params* r, int32_t head_dim) {
   if (!r->inv_freq || !aligned(r->inv_freq, 8)) return SEER_ERR_INVALID_ARG;
   if (r->rot_dim <= 0 || r->rot_dim > head_dim) return SEER_ERR_INVALID_ARG;
@@ -73,8 +81,8 @@ seer_status check_paged(const seer_paged_desc* d) {
   if (s == SEER_OK) s = check_pages(d->page_size, d->num_pages, d->batch, d->max_pages, d->table_stride);
   if (s == SEER_OK) s = check_strides(d->q_stride, d->dtype);
   if (s == SEER_OK) s = check_written(d->o_stride, {d->batch, d->heads_q, d->tokens}, d->head_dim, d->dtype);
-  if (s == SEER_OK) s = check_strides(d->k_cache_stride, d->dtype);
-  if (s == SEER_OK) s = check_strides(d->v_cache_stride, d->dtype);
+  if (s == SEER_OK) s = check_cache_strides(d->k_cache_stride, d->dtype);
+  if (s == SEER_OK) s = check_cache_strides(d->v_cache_stride, d->dtype);
   if (s != SEER_OK) return s;
   const int64_t rows = (int64_t)d->heads_q / d->heads_kv * d->tokens;
   if (rows > kMostTokens || (int64_t)d->batch * d->heads_kv > kMostTokens ||

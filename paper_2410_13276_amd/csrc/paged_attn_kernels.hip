@@ -35,13 +35,18 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kWorkers = 768;   // workgroups at most: three for each CU
-constexpr int kMinUnits = 2;    // units a workgroup has at least, where there are several
+constexpr int kWorkers = 512;   // workgroups at most: two for each CU
+constexpr int kRowCost = 1;     // a row's beginning and end, in units: what it weighs beside its units
 constexpr int kWholeKeys = 512; // caches of at most this many tokens a sequence are never split
 constexpr float kLn2 = 0.6931471805599453f;
 
+struct Stride16 {
+  uint32_t page, slot;
+};
+
 struct KernelArgs {
   PagedArgs a;
+  Stride16 kst, vst;            // strides of the pools, in 16-byte pieces
   int group, rows, row_blocks;  // G, G tokens, blocks of 16 NT rows
   int capacity;                 // tokens that a table row has room for
   int unit;                     // keys per unit
@@ -75,20 +80,64 @@ __device__ __forceinline__ int length_of(const KernelArgs& k, int b) {
   for (int s = 0; s < k.a.tokens; ++s) len = max(len, min(p[s], k.capacity - 1) + 1);
   return len;
 }
-__device__ __forceinline__ int units_of(const KernelArgs& k, int b) {
-  return max(1, (int)(((int64_t)length_of(k, b) + k.unit - 1) / k.unit));
+__device__ __forceinline__ int units_of(const KernelArgs& k, int len) {
+  return max(1, (int)(((uint32_t)len + (uint32_t)k.unit - 1u) / (uint32_t)k.unit));
 }
 
-// The units dealt to the workgroups: workgroup w has base (+ 1 for the first `rest`).
+// The weights dealt to the workgroups: workgroup w has base (+ 1 for the first `rest`).
 struct Deal {
   int64_t base, rest;
   int workers;
+  static __device__ __forceinline__ int64_t quot(int64_t x, int64_t y) {  // (64-bit division takes some 150 instructions)
+    return (x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
+  }
+  __device__ __forceinline__ Deal(int64_t total, int groups) {
+    workers = (int)min((int64_t)groups, total);
+    base = quot(total, workers);
+    rest = total - base * workers;
+  }
   __device__ __forceinline__ int64_t first(int w) const { return w * base + min((int64_t)w, rest); }
   __device__ __forceinline__ int owner(int64_t x) const {
     const int64_t big = rest * (base + 1);
-    return (int)(x < big ? x / (base + 1) : rest + (x - big) / base);
+    return (int)(x < big ? quot(x, base + 1) : rest + quot(x - big, base));
   }
 };
+
+__device__ __forceinline__ void unpack8(const u32x4 (&q)[1], float (&y)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    y[2 * i] = __uint_as_float(q[0][i] << 16);
+    y[2 * i + 1] = __uint_as_float(q[0][i] & 0xffff0000u);
+  }
+}
+__device__ __forceinline__ void unpack8(const u32x4 (&q)[2], float (&y)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(q[i / 4][i % 4]);
+}
+
+// Elements d0 .. d0 + 7 of a head, y, rotated at position pos; z: the other half of their planes (half layout).
+__device__ __forceinline__ void rotate8(const RopeView& r, const TurnRate* rate, int d0, int pos, float (&y)[8],
+                                        const float (&z)[8]) {
+  const bool second = d0 >= r.rot / 2;
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    float co[2], si[2];
+    if (r.interleaved) {
+      turn_cos_sin(rate[(d0 + i) / 2], pos, co[0], si[0]);
+      co[0] *= r.scale;
+      si[0] *= r.scale;
+      const float u = y[i], v = y[i + 1];
+      y[i] = u * co[0] - v * si[0];
+      y[i + 1] = u * si[0] + v * co[0];
+    } else {
+#pragma unroll
+      for (int f = 0; f < 2; ++f) {
+        turn_cos_sin(rate[(second ? d0 - r.rot / 2 : d0) + i + f], pos, co[f], si[f]);
+        y[i + f] = y[i + f] * (co[f] * r.scale) + z[i + f] * ((second ? si[f] : -si[f]) * r.scale);
+      }
+    }
+  }
+}
 
 // A tile's operands as a lane holds them.
 template <typename T, int D>
@@ -100,17 +149,20 @@ struct Tile {
 };
 
 template <typename T, int D, int NT, int QP, bool OCT>
-__global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
+__global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) {
   using S = Shape<T, D>;
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NA = D / 16;          // accumulators of a column tile
   constexpr int ROWS = 16 * NT;
   constexpr int OSTR = D + 4;
-  __shared__ __attribute__((aligned(16))) float sO[kWaves][ROWS][OSTR];
+  constexpr int QJ = BF ? D / 32 : D / 16;
+  // the operand Q^T as the lanes read it, then the wavefronts' results
+  __shared__ union {
+    u32x4 q[QP][NT][QJ][kWave];
+    float o[kWaves][ROWS][OSTR];
+  } sh;
   __shared__ float sM[kWaves][ROWS], sL[kWaves][ROWS];
-  __shared__ int sScan[kWaves];
-  __shared__ int sB;
-  __shared__ int64_t sOff;
+  __shared__ TurnRate sRate[64];
 
   const PagedArgs& a = ka.a;
   const int tid = threadIdx.x, lane = tid % kWave;
@@ -119,171 +171,239 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
   const int items = a.heads_kv * ka.row_blocks;  // rows of a sequence
   const float c = ka.scale_log2;
 
-  // ---- this workgroup's run of units
-  const int share = (a.batch + kThreads - 1) / kThreads;  // sequences per thread
-  const int b_lo = min(tid * share, a.batch), b_hi = min(b_lo + share, a.batch);
-  int mine = 0;
-  for (int b = b_lo; b < b_hi; ++b) mine += units_of(ka, b);
-  int upto = mine;  // inclusive prefix over the threads
+  const bool rope = a.rope.freq != nullptr;
+  if (rope && tid < a.rope.rot / 2) sRate[tid] = turn_rate(a.rope.freq[tid]);
+
+  // ---- this workgroup's share.  Every wavefront works it out by itself: a lane sums the weights of some
+  // sequences in a row, and a scan over the lanes finds the sequence that the share begins in.
+  const int share = (a.batch + kWave - 1) / kWave;  // sequences per lane
+  const int b_lo = min(lane * share, a.batch), b_hi = min(b_lo + share, a.batch);
+  int mine = 0, my_len = 0;
+  for (int i = b_lo; i < b_hi; ++i) {
+    my_len = length_of(ka, i);
+    mine += units_of(ka, my_len) + kRowCost;
+  }
+  int upto = mine;  // inclusive prefix over the lanes
 #pragma unroll
   for (int off = 1; off < kWave; off <<= 1) {
     const int y = __shfl_up(upto, off);
     if (lane >= off) upto += y;
   }
-  if (lane == kWave - 1) sScan[wave] = upto;
-  __syncthreads();
-  int all = 0;
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wave) upto += sScan[w];
-    all += sScan[w];
-  }
-  const int64_t total = (int64_t)all * items;
-  Deal deal;
-  deal.workers = (int)max((int64_t)1, min((int64_t)gridDim.x, total / kMinUnits));
-  if (!ka.join) deal.workers = (int)min((int64_t)gridDim.x, total);
   const int w = blockIdx.x;
+  const Deal deal((int64_t)__builtin_amdgcn_readlane(upto, kWave - 1) * items, (int)gridDim.x);
   if (w >= deal.workers) return;
-  deal.base = total / deal.workers;
-  deal.rest = total - deal.base * deal.workers;
   int64_t x = deal.first(w);
   const int64_t x_end = deal.first(w + 1);
-  {
-    int64_t before = (int64_t)(upto - mine) * items;
-    if (x >= before && x < (int64_t)upto * items) {
-      int b = b_lo;
-      for (; b < b_hi - 1; ++b) {
-        const int64_t next = before + (int64_t)units_of(ka, b) * items;
-        if (x < next) break;
-        before = next;
-      }
-      sB = b;
-      sOff = x - before;
-    }
+  const int owner_lane = (int)__popcll(__ballot((int64_t)upto * items <= x));
+  int b = owner_lane * share;
+  int64_t off = x - (int64_t)(__builtin_amdgcn_readlane(upto, owner_lane) - __builtin_amdgcn_readlane(mine, owner_lane)) * items;
+  int len = share == 1 ? __builtin_amdgcn_readlane(my_len, owner_lane) : length_of(ka, b);
+  int row_units = units_of(ka, len);
+  while (off >= (int64_t)(row_units + kRowCost) * items) {
+    off -= (int64_t)(row_units + kRowCost) * items;
+    len = length_of(ka, ++b);
+    row_units = units_of(ka, len);
   }
-  __syncthreads();
-  int b = sB;
-  int row_units = units_of(ka, b);
-  int item = (int)(sOff / row_units);
-  int u0 = (int)(sOff - (int64_t)item * row_units);
-  bool first_run = true;
+  len = __builtin_amdgcn_readfirstlane(len);
+  row_units = __builtin_amdgcn_readfirstlane(row_units);
+  int item = (int)off / (row_units + kRowCost);      // (off is below 2^30)
+  int at_w = (int)off - item * (row_units + kRowCost);  // position within the row's weight
 
-  for (; x < x_end;) {
-    const int take = (int)min((int64_t)(row_units - u0), x_end - x);
-    const int h = item / ka.row_blocks, rb = item - h * ka.row_blocks;
-    const int r0 = rb * ROWS;                      // the first row of the block
-    const int nrows = min(ROWS, ka.rows - r0);
-    const bool whole = take == row_units;
+  // ---- a run of one row's units [u0, u1): where it is, and its first tile
+  int u0, u1, h, key0, k_hi;
+  const char *kbase, *vbase;
+  const int32_t* table;
+
+  // The pages of a lane's keys of a tile, fetched a tile ahead of its loads.  K: lane row n
+  // of sub-tile i is key 8 (n / 4) + 4 i + n % 4 (bf16), n (fp32); V: keys PK g + e.  Where pages hold
+  // whole aligned runs of 8 keys (OCT) one look-up serves a run.
+  const int kk = BF ? n / 4 * 8 + n % 4 : n;
+  const int vk = S::PK * g;
+  struct Pages {
+    int k[OCT ? 1 : S::KSUB], v[OCT ? 1 : S::PK];
+  };
+  // (A key past the run is looked up at the run's last one and then has no page: no branch, and loads that are
+  // not wanted all go to the pool's first slots.)
+  auto page_of = [&](int key) -> int {
+    const int page = table[fast_quot(a.table.page, max(min(key, k_hi - 1), 0))];
+    return key < k_hi ? page : -1;
+  };
+  auto pages = [&](int key0) -> Pages {
+    Pages p;
+    if constexpr (OCT) {
+      p.k[0] = page_of(key0 + kk / 8 * 8);  // (the run's first key: it exists where any of them does)
+      p.v[0] = page_of(key0 + vk / 8 * 8);
+    } else {
+#pragma unroll
+      for (int i = 0; i < S::KSUB; ++i) p.k[i] = page_of(key0 + kk + 4 * i);
+#pragma unroll
+      for (int e = 0; e < S::PK; ++e) p.v[e] = page_of(key0 + vk + e);
+    }
+    return p;
+  };
+  // Address of a lane's piece of a key of page `page` (the pool's first slot where that is none).  Strides are
+  // counted in 16-byte pieces: two 32-bit multiplications make the offset.
+  auto place = [&](const char* base, const Stride16& t, int page, int key) -> const char* {
+    const bool ok = (uint32_t)page < (uint32_t)a.table.num_pages;
+    const int slot = key - fast_quot(a.table.page, key) * a.table.page.d;
+    const uint64_t off = (uint64_t)(uint32_t)(ok ? page : 0) * t.page + (uint64_t)(uint32_t)(ok ? slot : 0) * t.slot;
+    return base + (off << 4);
+  };
+
+  Tile<T, D> t;
+  auto load_k = [&](const Pages& pg, int key0) {
+#pragma unroll
+    for (int i = 0; i < S::KSUB; ++i) {
+      const char* p;
+      if constexpr (OCT) p = place(kbase, ka.kst, pg.k[0], key0 + kk) + 4 * i * ((uint64_t)ka.kst.slot << 4);
+      else p = place(kbase, ka.kst, pg.k[i], key0 + kk + 4 * i);
+#pragma unroll
+      for (int j = 0; j < S::KCH; ++j) t.k[i][j] = *(const u32x4*)(p + 64 * j);
+    }
+  };
+  auto load_v = [&](const Pages& pg, int key0) {
+    const char* p0;
+    t.there = 0;
+    if constexpr (OCT) {
+      p0 = place(vbase, ka.vst, pg.v[0], key0 + vk);
+      t.there = (uint32_t)pg.v[0] < (uint32_t)a.table.num_pages ? (1u << min(max(k_hi - (key0 + vk), 0), S::PK)) - 1u : 0u;
+    }
+#pragma unroll
+    for (int e = 0; e < S::PK; ++e) {
+      const char* p;
+      if constexpr (OCT) {
+        p = p0 + e * ((uint64_t)ka.vst.slot << 4);
+      } else {
+        const int page = pg.v[e];
+        p = place(vbase, ka.vst, page, key0 + vk + e);
+        t.there |= ((uint32_t)page < (uint32_t)a.table.num_pages ? 1u : 0u) << e;
+      }
+      if constexpr (BF && S::VW == 4) {
+        const u32x4 z = *(const u32x4*)p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) t.v[e][i] = z[i];
+      } else if constexpr (BF) {
+        const u32x2 z = *(const u32x2*)p;
+        t.v[e][0] = z[0];
+        t.v[e][1] = z[1];
+      } else {
+#pragma unroll
+        for (int f = 0; f < S::VP; ++f) {
+          const u32x4 z = *(const u32x4*)(p + 256 * f);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) t.v[e][4 * f + i] = z[i];
+        }
+      }
+    }
+  };
+
+  constexpr int STEP = kWaves * S::KT;
+  Pages pn;  // of the tile after the one that is loaded
+  // Q^T: a thread brings (and rotates) 8 elements at a time, QN times
+  constexpr int QN = (ROWS * (D / 8) + kThreads - 1) / kThreads;
+  constexpr int QW = BF ? 1 : 2;  // 16-byte pieces of 8 elements
+  u32x4 q_own[QN][QW], q_other[QN][QW];
+  int q_pos[QN];
+  // The next run of the share, with its first tile on the way; false when the share is done.
+  auto begin = [&]() -> bool {
+    for (;;) {
+      if (x >= x_end) return false;
+      const int take = (int)min((int64_t)(row_units + kRowCost - at_w), x_end - x);
+      u0 = max(at_w - kRowCost, 0);
+      u1 = max(at_w + take - kRowCost, 0);
+      if (u1 > u0) break;
+      x += take;  // (a row's cost alone)
+      at_w += take;
+    }
+    h = item / ka.row_blocks;
+    key0 = (int)min((int64_t)u0 * ka.unit, (int64_t)len) + wave * S::KT;
+    k_hi = (int)min((int64_t)u1 * ka.unit, (int64_t)len);
+    // a lane's piece of a K row: 16 bytes at 16 g of each 64; of a V row: 16 (8: bf16 of head_dim 64) at its share n
+    kbase = (const char*)((const T*)a.kc.ptr + h * a.kc.sh) + 16 * g;
+    vbase = (const char*)((const T*)a.vc.ptr + h * a.vc.sh) + (BF ? 4 * S::VW : 16) * n;
+    table = a.table.ptr + b * a.table.stride;
+    const Pages pg = pages(key0);
+    pn = pages(key0 + STEP);
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+      const int e = tid + i * kThreads, rl = e / (D / 8), d0 = e % (D / 8) * 8;
+      const int r = min((item - h * ka.row_blocks) * ROWS + rl, ka.rows - 1), tk = r / ka.group;
+      const T* src = (const T*)a.q.ptr + b * a.q.sb + (h * ka.group + (r - tk * ka.group)) * a.q.sh + tk * a.q.ss;
+      const int half = a.rope.rot / 2;
+      const bool turns = rope && d0 < a.rope.rot;
+      if (turns) q_pos[i] = a.positions[b * a.pos_stride + tk];
+      const T* other = src + (turns && !a.rope.interleaved ? (d0 < half ? d0 + half : d0 - half) : d0);
+#pragma unroll
+      for (int f = 0; f < QW; ++f) {
+        q_own[i][f] = *(const u32x4*)((const char*)(src + d0) + 16 * f);
+        if (QP == 2 || !BF) q_other[i][f] = *(const u32x4*)((const char*)other + 16 * f);
+      }
+    }
+    load_k(pg, key0);
+    load_v(pg, key0);
+    return true;
+  };
+  bool busy = begin();
+  bool first_run = true;
+  if (rope) __syncthreads();  // sRate is set
+
+  while (busy) {
+    const int r0 = (item - h * ka.row_blocks) * ROWS;  // the first row of the block
     const int32_t* pos_b = a.positions + b * a.pos_stride;
+
+    // ---- Q^T to LDS
+#pragma unroll
+    for (int i = 0; i < QN; ++i) {
+      const int e = tid + i * kThreads, rl = e / (D / 8), d0 = e % (D / 8) * 8;
+      if (rl >= ROWS) break;
+      const bool turns = rope && d0 < a.rope.rot;
+      if constexpr (BF) {
+        const int j = d0 / 32, at = d0 % 32 / 8 * 16 + rl % 16;
+        if constexpr (QP == 2) {
+          float y[8], z[8];
+          unpack8(q_own[i], y);
+          unpack8(q_other[i], z);
+          if (turns) rotate8(a.rope, sRate, d0, q_pos[i], y, z);
+          bf16x8 hi, lo;
+#pragma unroll
+          for (int f = 0; f < 8; ++f) {
+            hi[f] = (__bf16)y[f];
+            lo[f] = (__bf16)(y[f] - (float)hi[f]);
+          }
+          sh.q[0][rl / 16][j][at] = __builtin_bit_cast(u32x4, hi);
+          sh.q[QP - 1][rl / 16][j][at] = __builtin_bit_cast(u32x4, lo);
+        } else {
+          sh.q[0][rl / 16][j][at] = q_own[i][0];
+        }
+      } else {
+        const int j = d0 / 16, at = d0 % 16 / 4 * 16 + rl % 16;
+        float y[8], z[8];
+        unpack8(q_own[i], y);
+        unpack8(q_other[i], z);
+        if (turns) rotate8(a.rope, sRate, d0, q_pos[i], y, z);
+#pragma unroll
+        for (int f = 0; f < 2; ++f)
+          sh.q[0][rl / 16][j][at + 16 * f] = u32x4{__float_as_uint(y[4 * f]), __float_as_uint(y[4 * f + 1]),
+                                                   __float_as_uint(y[4 * f + 2]), __float_as_uint(y[4 * f + 3])};
+      }
+    }
 
     // ---- the columns: rows r0 + 16 ct + n, the last key each sees
     int last[NT], token[NT];
-    int most = -1, least = 0x7fffffff;
-    const T* qp[NT];
+    int least = 0x7fffffff;
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) {
       const int r = min(r0 + 16 * ct + n, ka.rows - 1);
-      const int t = r / ka.group;
-      token[ct] = t;
-      const int p = min(pos_b[t], ka.capacity - 1);
-      last[ct] = p;
-      most = max(most, p);
-      if (p >= 0) least = min(least, p);
-      qp[ct] = (const T*)a.q.ptr + b * a.q.sb + (h * ka.group + (r - t * ka.group)) * a.q.sh + t * a.q.ss;
+      token[ct] = r / ka.group;
+      last[ct] = min(pos_b[token[ct]], ka.capacity - 1);
+      if (last[ct] >= 0) least = min(least, last[ct]);
     }
 #pragma unroll
-    for (int off = 1; off < 16; off <<= 1) {
-      most = max(most, __shfl_xor(most, off));
-      least = min(least, __shfl_xor(least, off));
-    }
-    const int len = __builtin_amdgcn_readfirstlane(most + 1);
-    const int common = __builtin_amdgcn_readfirstlane(most < 0 ? 0 : least + 1);  // keys that every live row sees
-    const int64_t k_lo = (int64_t)u0 * ka.unit;
-    const int k_hi = (int)min((int64_t)len, k_lo + (int64_t)take * ka.unit);
-    // tiles below `even` are seen alike by all live rows
+    for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
+    // keys below `even` are seen alike by all live rows (where no row is live, none matters)
+    const int common = __builtin_amdgcn_readfirstlane(least) < len ? __builtin_amdgcn_readfirstlane(least) + 1 : len;
     const int even = common == len ? k_hi : min(k_hi, common / S::KT * S::KT);
-
-    // ---- Q^T operand, in QP parts
-    constexpr int QJ = BF ? D / 32 : D / 16;
-    u32x4 q[QP][NT][QJ];
-    if (a.rope.freq != nullptr) {
-      // a thread rotates 8 elements of one row, then the operands are read back
-      for (int e = tid; e < ROWS * (D / 8); e += kThreads) {
-        const int rl = e / (D / 8), d0 = e % (D / 8) * 8;
-        const int r = min(r0 + rl, ka.rows - 1), t = r / ka.group;
-        const T* src = (const T*)a.q.ptr + b * a.q.sb + (h * ka.group + (r - t * ka.group)) * a.q.sh + t * a.q.ss;
-        const int half = a.rope.rot / 2;
-        const int pos = pos_b[t];
-        const bool turns = d0 < a.rope.rot, second = d0 >= half;
-        float own[8], other[8];
-        auto load8 = [&](int d, float(&y)[8]) {
-          if constexpr (BF) {
-            const u32x4 z = *(const u32x4*)(src + d);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              y[2 * i] = __uint_as_float(z[i] << 16);
-              y[2 * i + 1] = __uint_as_float(z[i] & 0xffff0000u);
-            }
-          } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = src[d + i];
-          }
-        };
-        load8(d0, own);
-        if (turns) {
-          if (a.rope.interleaved) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              float co, si;
-              turn_cos_sin(turn_rate(a.rope.freq[d0 / 2 + i]), pos, co, si);
-              co *= a.rope.scale;
-              si *= a.rope.scale;
-              const float u = own[2 * i], v = own[2 * i + 1];
-              own[2 * i] = u * co - v * si;
-              own[2 * i + 1] = u * si + v * co;
-            }
-          } else {
-            load8(second ? d0 - half : d0 + half, other);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              float co, si;
-              turn_cos_sin(turn_rate(a.rope.freq[(second ? d0 - half : d0) + i]), pos, co, si);
-              own[i] = own[i] * (co * a.rope.scale) + other[i] * ((second ? si : -si) * a.rope.scale);
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sO[0][rl][d0 + i] = own[i];
-      }
-      __syncthreads();
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-        for (int j = 0; j < QJ; ++j) {
-          if constexpr (BF) {
-            const float* z = &sO[0][16 * ct + n][32 * j + 8 * g];
-            union {
-              bf16x8 v;
-              u32x4 r;
-            } hi, lo;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-              hi.v[i] = (__bf16)z[i];
-              lo.v[i] = (__bf16)(z[i] - (float)hi.v[i]);
-            }
-            q[0][ct][j] = hi.r;
-            if constexpr (QP == 2) q[1][ct][j] = lo.r;
-          } else {
-            q[0][ct][j] = *(const u32x4*)&sO[0][16 * ct + n][16 * j + 4 * g];
-          }
-        }
-      __syncthreads();  // sO is free again
-    } else {
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-        for (int j = 0; j < QJ; ++j)
-          q[0][ct][j] = *(const u32x4*)(qp[ct] + (BF ? 32 * j + 8 * g : 16 * j + 4 * g));
-    }
+    __syncthreads();
 
     f32x4 acc[NT][NA];
 #pragma unroll
@@ -294,104 +414,33 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) m[ct] = -INFINITY, l[ct] = 0.f;
 
-    const T* kbase = (const T*)a.kc.ptr + h * a.kc.sh;
-    const T* vbase = (const T*)a.vc.ptr + h * a.vc.sh;
-    const int32_t* table = a.table.ptr + b * a.table.stride;
-
-    // page and slot of a key; false (page 0, slot 0) where there is none
-    auto find = [&](int key, int64_t& page, int64_t& slot) -> bool {
-      const int i = fast_quot(a.table.page, key);
-      const int p = key < len ? table[i] : -1;
-      const bool ok = p >= 0 && p < a.table.num_pages;
-      page = ok ? p : 0;
-      slot = ok ? key - i * a.table.page.d : 0;
-      return ok;
-    };
-
-    using TileT = Tile<T, D>;
-    auto load = [&](TileT& t, int key0) {
-      // K: lane row r = n of sub-tile i is key 8 (r / 4) + 4 i + r % 4 (bf16), r (fp32)
-      const int kk = BF ? n / 4 * 8 + n % 4 : n;
-      const T* kp[S::KSUB];
-      if constexpr (OCT) {  // pages hold whole aligned runs of 8 keys: one look-up for each run
-        int64_t page, slot;
-        find(key0 + kk / 8 * 8, page, slot);
-#pragma unroll
-        for (int i = 0; i < S::KSUB; ++i) kp[i] = kbase + page * a.kc.sp + (slot + kk % 8 + 4 * i) * a.kc.ss;
-      } else {
-#pragma unroll
-        for (int i = 0; i < S::KSUB; ++i) {
-          int64_t page, slot;
-          find(key0 + kk + 4 * i, page, slot);
-          kp[i] = kbase + page * a.kc.sp + slot * a.kc.ss;
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < S::KSUB; ++i)
-#pragma unroll
-        for (int j = 0; j < S::KCH; ++j) t.k[i][j] = *(const u32x4*)(kp[i] + (BF ? 32 * j + 8 * g : 16 * j + 4 * g));
-      // V: the lane's keys are PK g + e
-      const int vk = S::PK * g;
-      t.there = 0;
-      const T* vp = vbase;
-      if constexpr (OCT) {
-        int64_t page, slot;
-        const bool ok = find(key0 + vk / 8 * 8, page, slot);
-        vp = vbase + page * a.vc.sp + (slot + vk % 8) * a.vc.ss;
-        if (ok) {
-          const int seen = min(max(len - (key0 + vk), 0), S::PK);
-          t.there = (1u << seen) - 1u;
-        }
-      }
-#pragma unroll
-      for (int e = 0; e < S::PK; ++e) {
-        const T* p = vp + e * a.vc.ss;
-        if constexpr (!OCT) {
-          int64_t page, slot;
-          if (find(key0 + vk + e, page, slot)) t.there |= 1u << e;
-          p = vbase + page * a.vc.sp + slot * a.vc.ss;
-        }
-        if constexpr (BF && S::VW == 4) {
-          const u32x4 z = *(const u32x4*)(p + 8 * n);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) t.v[e][i] = z[i];
-        } else if constexpr (BF) {
-          const u32x2 z = *(const u32x2*)(p + 4 * n);
-          t.v[e][0] = z[0];
-          t.v[e][1] = z[1];
-        } else {
-#pragma unroll
-          for (int f = 0; f < S::VP; ++f) {
-            const u32x4 z = *(const u32x4*)(p + 64 * f + 4 * n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) t.v[e][4 * f + i] = z[i];
-          }
-        }
-      }
-    };
-
     // S^T of a column tile: element e is key key0 + PK g + e of the lane's column
-    auto scores = [&](const TileT& t, int ct, float (&s)[S::PK]) {
+    auto scores = [&](int ct, int at, float (&s)[S::PK]) {
+      f32x4 y[S::KSUB];
 #pragma unroll
-      for (int i = 0; i < S::KSUB; ++i) {
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < S::KSUB; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int part = QP - 1; part >= 0; --part)
+      for (int part = QP - 1; part >= 0; --part)
 #pragma unroll
-          for (int j = 0; j < S::KCH; ++j) {
+        for (int j = 0; j < S::KCH; ++j) {
+          const u32x4 q = sh.q[part][ct][j][at];
+#pragma unroll
+          for (int i = 0; i < S::KSUB; ++i) {
             if constexpr (BF) {
-              y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[i][j]),
-                                                          __builtin_bit_cast(bf16x8, q[part][ct][j]), y, 0, 0, 0);
+              y[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, t.k[i][j]),
+                                                             __builtin_bit_cast(bf16x8, q), y[i], 0, 0, 0);
             } else {
 #pragma unroll
               for (int f = 0; f < 4; ++f)
-                y = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][f]),
-                                                         __uint_as_float(q[part][ct][j][f]), y, 0, 0, 0);
+                y[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][f]), __uint_as_float(q[f]), y[i],
+                                                            0, 0, 0);
             }
           }
+        }
 #pragma unroll
-        for (int f = 0; f < 4; ++f) s[4 * i + f] = y[f];
-      }
+      for (int i = 0; i < S::KSUB; ++i)
+#pragma unroll
+        for (int f = 0; f < 4; ++f) s[4 * i + f] = y[i][f];
     };
 
     // running maximum and sum; s becomes P
@@ -420,93 +469,141 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
       }
     };
 
-    // o += V^T P^T; accumulator i, element f of the lane: column n, feature
-    // (4 g + f) D/16 + i (bf16), 64 (i / 4) + 4 (4 g + f) + i % 4 (fp32)
-    auto product = [&](const TileT& t, const float (&p)[S::PK], f32x4 (&o)[NA]) {
+    // P^T as the operand of the second product (bf16: in two parts)
+    struct Weights {
+      bf16x8 hi, lo;
+      float p[S::PK];
+    };
+    auto weights = [&](const float (&p)[S::PK]) -> Weights {
+      Weights w;
       if constexpr (BF) {
-        bf16x8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-          hi[e] = (__bf16)p[e];
-          lo[e] = (__bf16)(p[e] - (float)hi[e]);
-        }
-#pragma unroll
-        for (int i = 0; i < NA; ++i) {
-          u32x4 z;
-#pragma unroll
-          for (int f = 0; f < 4; ++f)
-            z[f] = __builtin_amdgcn_perm(t.v[2 * f + 1][i / 2], t.v[2 * f][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
-          const bf16x8 vt = __builtin_bit_cast(bf16x8, z);
-          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, lo, o[i], 0, 0, 0);
-          o[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, hi, o[i], 0, 0, 0);
+          w.hi[e] = (__bf16)p[e];
+          w.lo[e] = (__bf16)(p[e] - (float)w.hi[e]);
         }
       } else {
 #pragma unroll
-        for (int e = 0; e < S::PK; ++e)
+        for (int e = 0; e < S::PK; ++e) w.p[e] = p[e];
+      }
+      return w;
+    };
+    // y + V^T P^T of accumulator i, the bits outside `keep` taken as 0.  Element f of the
+    // lane: column n, feature (4 g + f) D / 16 + i (bf16), 64 (i / 4) + 4 (4 g + f) + i % 4 (fp32)
+    auto product = [&](const Weights& w, int i, f32x4 y, const uint32_t (&keep)[4]) -> f32x4 {
+      if constexpr (BF) {
+        u32x4 z;
 #pragma unroll
-          for (int i = 0; i < NA; ++i)
-            o[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[e][i]), p[e], o[i], 0, 0, 0);
+        for (int f = 0; f < 4; ++f)
+          z[f] = keep[f] & __builtin_amdgcn_perm(t.v[2 * f + 1][i / 2], t.v[2 * f][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+        const bf16x8 vt = __builtin_bit_cast(bf16x8, z);
+        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w.lo, y, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w.hi, y, 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int e = 0; e < S::PK; ++e)
+          y = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.v[e][i] & keep[e]), w.p[e], y, 0, 0, 0);
+        return y;
       }
     };
 
-    constexpr int STEP = kWaves * S::KT;
-    int key0 = (int)k_lo + wave * S::KT;
+    // the bits of V's operands that belong to the keys in `seen`
+    auto mask = [&](uint32_t seen, uint32_t (&keep)[4]) {
+#pragma unroll
+      for (int f = 0; f < 4; ++f) {
+        if constexpr (BF) keep[f] = (seen >> 2 * f & 1 ? 0xffffu : 0u) | (seen >> (2 * f + 1) & 1 ? 0xffff0000u : 0u);
+        else keep[f] = seen >> f & 1 ? ~0u : 0u;
+      }
+    };
+
+    // Tiles that all live rows see alike.  A tile's K registers take the next tile's keys as soon as its scores are
+    // formed, its V registers after the second product, so that loads are always in flight; pages are looked up
+    // two tiles ahead (loads return in order: a look-up behind a tile's loads would wait for them).
+    int at = lane;
     for (; key0 < even; key0 += STEP) {
-      TileT t;
-      load(t, key0);
-      const bool full = __ballot(t.there != (1u << S::PK) - 1u) == 0;
-      if (!full) {  // what stands in slots that no row sees may be anything
+      asm volatile("" : "+v"(at));  // (the reads of Q^T stay in the loop: kept in registers, they would spill)
+      float s[NT][S::PK];
 #pragma unroll
-        for (int e = 0; e < S::PK; ++e)
-          if (!(t.there >> e & 1))
-#pragma unroll
-            for (int i = 0; i < S::VW; ++i) t.v[e][i] = 0;
-      }
+      for (int ct = 0; ct < NT; ++ct) scores(ct, at, s[ct]);
+      __builtin_amdgcn_sched_barrier(0);  // (the next keys take the registers of these)
+      const Pages pg = pn;
+      pn = pages(key0 + 2 * STEP);
+      load_k(pg, key0 + STEP);
+      // (what stands in slots that no row sees may be anything: always masked, which the loads' time hides)
+      uint32_t keep[4];
+      mask(t.there, keep);
+      Weights w[NT];
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
-        float s[S::PK];
-        scores(t, ct, s);
-        if (!full)
 #pragma unroll
-          for (int e = 0; e < S::PK; ++e) s[e] = t.there >> e & 1 ? s[e] : -INFINITY;
-        softmax(ct, s);
-        product(t, s, acc[ct]);
+        for (int e = 0; e < S::PK; ++e) s[ct][e] = t.there >> e & 1 ? s[ct][e] : -INFINITY;
+        softmax(ct, s[ct]);
+        w[ct] = weights(s[ct]);
       }
+#pragma unroll
+      for (int i = 0; i < NA; ++i)
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) acc[ct][i] = product(w[ct], i, acc[ct][i], keep);
+      __builtin_amdgcn_sched_barrier(0);  // (as above, for V)
+      load_v(pg, key0 + STEP);
     }
-    // the keys near the new tokens, where the tokens' rows see different ones: a key that
-    // one token does not see must not reach its output even as 0 times whatever V holds
+    // The keys near the new tokens, whose rows see different ones: one that a token does not see must not
+    // reach its output even as 0 times whatever V holds.
     for (; key0 < k_hi; key0 += STEP) {
-      TileT t;
-      load(t, key0);
-      const int lane_key = key0 + S::PK * g;
+      const int lane_key = key0 + vk;
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
         float s[S::PK];
-        scores(t, ct, s);
+        scores(ct, lane, s);
 #pragma unroll
-        for (int e = 0; e < S::PK; ++e)
-          s[e] = (t.there >> e & 1) && lane_key + e <= last[ct] ? s[e] : -INFINITY;
+        for (int e = 0; e < S::PK; ++e) s[e] = (t.there >> e & 1) && lane_key + e <= last[ct] ? s[e] : -INFINITY;
         softmax(ct, s);
-        const int t_lo = min(r0 + 16 * ct, ka.rows - 1) / ka.group, t_hi = min(r0 + 16 * ct + 15, ka.rows - 1) / ka.group;
+        const Weights w = weights(s);
+        const int t_lo = min(r0 + 16 * ct, ka.rows - 1) / ka.group;
+        const int t_hi = min(r0 + 16 * ct + 15, ka.rows - 1) / ka.group;
         for (int tk = t_lo; tk <= t_hi; ++tk) {
-          const int lk = min(pos_b[tk], ka.capacity - 1);
-          TileT seen;
+          const int end = max(min(pos_b[tk], ka.capacity - 1), -1) + 1;  // the token's keys
+          const uint32_t seen = t.there & ((1u << min(max(end - lane_key, 0), S::PK)) - 1u);
+          uint32_t keep[4];
+          mask(seen, keep);
 #pragma unroll
-          for (int e = 0; e < S::PK; ++e)
-#pragma unroll
-            for (int i = 0; i < S::VW; ++i) seen.v[e][i] = (t.there >> e & 1) && lane_key + e <= lk ? t.v[e][i] : 0;
-          f32x4 o[NA];
-#pragma unroll
-          for (int i = 0; i < NA; ++i) o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-          product(seen, s, o);
-          if (token[ct] == tk)
-#pragma unroll
-            for (int i = 0; i < NA; ++i) acc[ct][i] += o[i];
+          for (int i = 0; i < NA; ++i) {
+            __builtin_amdgcn_sched_barrier(0);  // (one at a time: side by side they would spill)
+            const f32x4 o = product(w, i, f32x4{0.f, 0.f, 0.f, 0.f}, keep);
+            if (token[ct] == tk) acc[ct][i] += o;
+          }
         }
+      }
+      if (key0 + STEP < k_hi) {
+        load_k(pn, key0 + STEP);
+        load_v(pn, key0 + STEP);
+        pn = pages(key0 + 2 * STEP);
       }
     }
 
+    // ---- the next run, its first tile in flight under this one's end
+    const int cur_b = b, cur_item = item, cur_h = h;
+    const bool opens = u0 == 0, whole = opens && u1 == row_units;
+    const int64_t row_last = x - at_w + row_units + kRowCost - 1;  // the row's last unit
+    const int done = u1 + kRowCost - at_w;
+    x += done;
+    at_w += done;
+    if (u1 == row_units) {
+      at_w = 0;
+      if (++item == items) {
+        item = 0;
+        ++b;
+        if (x < x_end) {
+          len = __builtin_amdgcn_readfirstlane(length_of(ka, b));
+          row_units = units_of(ka, len);
+        }
+      }
+    }
+    busy = begin();
+
     // ---- the wavefronts' results together
+    const int nrows = min(ROWS, ka.rows - r0);
+    __syncthreads();  // sh.q is read
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) {
       l[ct] += __shfl_xor(l[ct], 16);
@@ -516,12 +613,13 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
         sM[wave][col] = m[ct];
         sL[wave][col] = l[ct];
       }
+      if (col < nrows)
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
           const int d = BF ? (4 * g + f) * NA + i : 64 * (i / 4) + 4 * (4 * g + f) + i % 4;
-          sO[wave][col][d] = acc[ct][i][f];
+          sh.o[wave][col][d] = acc[ct][i][f];
         }
     }
     __syncthreads();
@@ -537,17 +635,17 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
       for (int i = 0; i < kWaves; ++i) {
         const float wgt = sM[i][rl] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((sM[i][rl] - mx) * c);
         sum += wgt * sL[i][rl];
-        o += wgt * *(const f32x4*)&sO[i][rl][d];
+        o += wgt * *(const f32x4*)&sh.o[i][rl][d];
       }
       if (!whole) {
         *(f32x4*)(ka.part_o + ((int64_t)slot * ROWS + rl) * D + d) = o;
         if (d == 0) ka.part_ml[(int64_t)slot * ROWS + rl] = make_float2(mx, sum);
         continue;
       }
-      const int r = r0 + rl, t = r / ka.group, hq = h * ka.group + (r - t * ka.group);
-      const bool none = sum == 0.f || pos_b[t] < 0;
+      const int r = r0 + rl, tk = r / ka.group, hq = cur_h * ka.group + (r - tk * ka.group);
+      const bool none = sum == 0.f || pos_b[tk] < 0;
       const float inv = none ? 0.f : 1.f / sum;
-      T* out = (T*)a.o + b * a.osb + hq * a.osh + t * a.oss + d;
+      T* out = (T*)a.o + cur_b * a.osb + hq * a.osh + tk * a.oss + d;
 #pragma unroll
       for (int f = 0; f < 4; ++f) {
         const float y = none ? 0.f : o[f] * inv;
@@ -555,36 +653,26 @@ __global__ __launch_bounds__(kThreads) void paged_attn_kernel(KernelArgs ka) {
         else out[f] = y;
       }
       if (a.lse != nullptr && d == 0)
-        a.lse[((int64_t)b * a.heads_q + hq) * a.tokens + t] =
+        a.lse[((int64_t)cur_b * a.heads_q + hq) * a.tokens + tk] =
             none ? -INFINITY : ((mx == -INFINITY ? 0.f : mx * c) + __log2f(sum)) * kLn2;
     }
-    if (ka.join && u0 == 0 && tid == 0)
-      ka.record[(int64_t)b * items + item] =
-          whole ? make_int2(-1, -1) : make_int2(slot, deal.owner(x + row_units - 1));
-    __syncthreads();
-
+    if (ka.join && opens && tid == 0)
+      ka.record[(int64_t)cur_b * items + cur_item] = whole ? make_int2(-1, -1) : make_int2(slot, deal.owner(row_last));
+    if (!busy) break;
     first_run = false;
-    x += take;
-    u0 += take;
-    if (u0 == row_units) {
-      u0 = 0;
-      if (++item == items) {
-        item = 0;
-        ++b;
-        if (x < x_end) row_units = units_of(ka, b);
-      }
-    }
+    __syncthreads();  // sh.o is read
   }
 }
 
-// One row (a token of a query head) whose keys several workgroups shared: their partial
-// results, in the order of the keys.
+// Rows whose keys several workgroups shared: their partial results, in the order of the keys.
+// A workgroup joins JR rows of an item; a thread sums 4 features over the parts grp, grp + GRP, ..
+constexpr int kJoinThreads = 256, kJoinRows = 4;
 template <typename T, int D>
-__global__ __launch_bounds__(kThreads) void paged_join_kernel(KernelArgs ka, int rows_block) {
-  constexpr int V4 = D / 4, GRP = kThreads / V4;
-  __shared__ float sW[kWorkers];
-  __shared__ float sR[kWaves], sS[kWaves];
-  __shared__ __attribute__((aligned(16))) float sO[GRP][D];
+__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka, int rows_block) {
+  constexpr int V4 = D / 4, GRP = kJoinThreads / (V4 * kJoinRows), AHEAD = 8;
+  __shared__ float sW[kJoinRows][kWorkers];
+  __shared__ float2 sT[kJoinRows];
+  __shared__ __attribute__((aligned(16))) float sO[GRP][kJoinRows][D];
   const PagedArgs& a = ka.a;
   const int64_t at = blockIdx.x;
   const int2 rec = ka.record[at];
@@ -592,51 +680,60 @@ __global__ __launch_bounds__(kThreads) void paged_join_kernel(KernelArgs ka, int
   const int items = a.heads_kv * ka.row_blocks;
   const int b = (int)(at / items), item = (int)(at - (int64_t)b * items);
   const int h = item / ka.row_blocks, rb = item - h * ka.row_blocks;
-  const int rl = blockIdx.y, r = rb * rows_block + rl;
-  if (r >= ka.rows) return;
-  const int w0 = rec.x / 2, parts = rec.y - w0 + 1;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  auto slot = [&](int p) { return (int64_t)(p == 0 ? rec.x : 2 * (w0 + p)) * rows_block + rl; };
+  const int nrows = min(rows_block, ka.rows - rb * rows_block);
+  const int w0 = rec.x / 2, parts = rec.y - w0 + 1;
+  auto slot = [&](int p, int rl) { return (int64_t)(p == 0 ? rec.x : 2 * (w0 + p)) * rows_block + rl; };
   const float c = ka.scale_log2;
 
-  float mx = -INFINITY;
-  for (int p = tid; p < parts; p += kThreads) mx = fmaxf(mx, ka.part_ml[slot(p)].x);
-  mx = wave_max(mx);
-  if (lane == 0) sR[wave] = mx;
-  __syncthreads();
+  // the first parts are on their way while the weights are formed
+  const int d = tid % V4 * 4, jr = tid / V4 % kJoinRows, grp = tid / (V4 * kJoinRows);
+  const int rl = min((int)blockIdx.y * kJoinRows + jr, nrows - 1);
+  auto part = [&](int p) { return *(const f32x4*)(ka.part_o + slot(p, rl) * D + d); };
+  f32x4 y[AHEAD];
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) mx = fmaxf(mx, sR[i]);
-  float sum = 0.f;
-  for (int p = tid; p < parts; p += kThreads) {
-    const float2 ml = ka.part_ml[slot(p)];
-    const float wgt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mx) * c);
-    sW[p] = wgt;
-    sum += wgt * ml.y;
-  }
-  sum = wave_sum(sum);
-  if (lane == 0) sS[wave] = sum;
-  __syncthreads();
-  sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i) sum += sS[i];
+  for (int i = 0; i < AHEAD; ++i) y[i] = part(min(grp + i * GRP, parts - 1));
 
-  const int d = tid % V4 * 4, grp = tid / V4;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int p = grp; p < parts; p += GRP) o += sW[p] * *(const f32x4*)(ka.part_o + slot(p) * D + d);
-  *(f32x4*)&sO[grp][d] = o;
-  __syncthreads();
-  const int t = r / ka.group, hq = h * ka.group + (r - t * ka.group);
-  const bool none = sum == 0.f || a.positions[b * a.pos_stride + t] < 0;
-  if (tid < D) {
-    float y = 0.f;
-#pragma unroll
-    for (int i = 0; i < GRP; ++i) y += sO[i][tid];
-    y = none ? 0.f : y / sum;
-    T* out = (T*)a.o + b * a.osb + hq * a.osh + t * a.oss + tid;
-    if constexpr (sizeof(T) == 2) *(__bf16*)out = (__bf16)y;
-    else *out = y;
+  static_assert(kJoinRows == kJoinThreads / kWave, "a wavefront forms one row's weights");
+  {
+    const int row = min((int)blockIdx.y * kJoinRows + wave, nrows - 1);
+    float mx = -INFINITY;
+    for (int p = lane; p < parts; p += kWave) mx = fmaxf(mx, ka.part_ml[slot(p, row)].x);
+    mx = wave_max(mx);
+    float sum = 0.f;
+    for (int p = lane; p < parts; p += kWave) {
+      const float2 ml = ka.part_ml[slot(p, row)];
+      const float wgt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mx) * c);
+      sW[wave][p] = wgt;
+      sum += wgt * ml.y;
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) sT[wave] = make_float2(mx, sum);
   }
-  if (a.lse != nullptr && tid == 0)
+  __syncthreads();
+
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i)
+    if (grp + i * GRP < parts) o += sW[jr][grp + i * GRP] * y[i];
+#pragma unroll 4
+  for (int p = grp + AHEAD * GRP; p < parts; p += GRP) o += sW[jr][p] * part(p);
+  *(f32x4*)&sO[grp][jr][d] = o;
+  __syncthreads();
+  if (grp != 0 || (int)blockIdx.y * kJoinRows + jr >= nrows) return;
+#pragma unroll
+  for (int i = 1; i < GRP; ++i) o += *(const f32x4*)&sO[i][jr][d];
+  const float mx = sT[jr].x, sum = sT[jr].y;
+  const int r = rb * rows_block + rl, t = r / ka.group, hq = h * ka.group + (r - t * ka.group);
+  const bool none = sum == 0.f || a.positions[b * a.pos_stride + t] < 0;
+  T* out = (T*)a.o + b * a.osb + hq * a.osh + t * a.oss + d;
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    const float z = none ? 0.f : o[f] / sum;
+    if constexpr (sizeof(T) == 2) ((__bf16*)out)[f] = (__bf16)z;
+    else out[f] = z;
+  }
+  if (a.lse != nullptr && d == 0)
     a.lse[((int64_t)b * a.heads_q + hq) * a.tokens + t] =
         none ? -INFINITY : ((mx == -INFINITY ? 0.f : mx * c) + __log2f(sum)) * kLn2;
 }
@@ -676,7 +773,7 @@ hipError_t launch_typed(const KernelArgs& k, int nt, dim3 grid, hipStream_t s) {
   }
   if (e != hipSuccess || !k.join) return e;
   const int64_t rows = (int64_t)k.a.batch * k.a.heads_kv * k.row_blocks;
-  paged_join_kernel<T, D><<<dim3((unsigned)rows, (unsigned)std::min(k.rows, 16 * nt)), kThreads, 0, s>>>(k, 16 * nt);
+  paged_join_kernel<T, D><<<dim3((unsigned)rows, (unsigned)((std::min(k.rows, 16 * nt) + kJoinRows - 1) / kJoinRows)), kJoinThreads, 0, s>>>(k, 16 * nt);
   return hipGetLastError();
 }
 
@@ -690,6 +787,9 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   const Plan p = plan(a.batch, a.heads_q, a.heads_kv, a.tokens, a.head_dim);
   KernelArgs k;
   k.a = a;
+  const int piece = a.bf16 ? 8 : 4;
+  k.kst = {(uint32_t)(a.kc.sp / piece), (uint32_t)(a.kc.ss / piece)};
+  k.vst = {(uint32_t)(a.vc.sp / piece), (uint32_t)(a.vc.ss / piece)};
   k.group = p.group;
   k.rows = p.rows;
   k.row_blocks = p.row_blocks;
@@ -701,7 +801,7 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   if (!k.join) unit = (k.capacity + step - 1) / step * step;
   // (counts of units stay below 2^31)
   auto units = [&]() { return (k.capacity + unit - 1) / unit; };
-  while (units() * std::max((int64_t)a.batch, items) > INT32_MAX / 2 && unit < (1 << 29)) unit *= 2;
+  while ((units() + kRowCost) * std::max((int64_t)a.batch, items) > INT32_MAX / 2 && unit < (1 << 29)) unit *= 2;
   k.unit = (int)unit;
   k.scale_log2 = a.scale * kLog2e;
   char* ws = (char*)a.workspace;

@@ -36,63 +36,75 @@ _ROPE_DESC = struct.Struct("=6i13q")   # seer_rope_desc
 _CACHE_DESC = struct.Struct("=10i14q")  # seer_append_desc, seer_paged_desc
 
 
-def _check_tensors(named, dtype):
-    """Same device (a GPU) and type, unit last stride; returns the device."""
-    device = named[0][1].device
-    for name, t in named:
-        if not t.is_cuda or t.device != device:
+# A call's checks cost the host more than its launch, so each call tests its conditions in one expression and only
+# looks for the one that failed, in these functions, when there is any.
+
+def _refuse_tensors(dtype, **named):
+    """Raises for the tensor (None: not given) that is not on the GPU of the first, of its type, with unit last stride."""
+    first = next(iter(named.values()))
+    for name, t in named.items():
+        if t is None:
+            continue
+        if not t.is_cuda or t.device != first.device:
             raise ValueError(f"{name} must be on the GPU of the other tensors")
         if t.dtype != dtype:
             raise TypeError(f"{name} must be {dtype} like the other tensors")
-        if t.shape[-1] > 1 and t.stride(-1) != 1:
+        if t.stride(-1) != 1:
             raise ValueError(f"{name} must have unit last stride")
-    return device
 
 
-def _check_ints(name, t, device, dims):
-    torch = _seer._torch()
-    if t.dtype != torch.int32:
+def _check_int(name, t, dev):
+    if t.dtype is not _t.int32:
         raise TypeError(f"{name} must be int32")
-    if t.device != device:
+    if t.get_device() != dev:
         raise ValueError(f"{name} must be on the GPU of the other tensors")
-    if t.dim() not in dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise ValueError(f"{name} must have {' or '.join(map(str, dims))} dimensions and unit last stride")
 
 
-def _rope_arg(inv_freq, interleaved, scale, device):
+def _rope_arg(inv_freq, interleaved, scale, dev):
     """seer_rope_params, or None without frequencies."""
     if inv_freq is None:
         return None
-    torch = _seer._torch()
-    if inv_freq.dtype != torch.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+    if inv_freq.dtype is not _t.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
         raise TypeError("inv_freq must be a contiguous float64 vector (rope_freqs)")
-    if inv_freq.device != device:
+    if inv_freq.get_device() != dev:
         raise ValueError("inv_freq must be on the GPU of the other tensors")
-    return _ROPE.pack(inv_freq.data_ptr(), 2 * inv_freq.shape[0], int(bool(interleaved)), float(scale))
+    return _ROPE.pack(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale)
 
 
-class _On:
-    """Makes a call's device and stream current (nothing to do where they are), so that memory which the call
-    allocates belongs to the stream that works on it."""
+_t = None          # torch, once a call has needed it
+_raw_stream = None  # device index -> handle of its current stream
 
-    def __init__(self, device, stream):
-        torch = _seer._torch()
-        self.guard = None
-        if stream is not None:
-            if stream.device != device:
-                raise ValueError("the stream belongs to another device than the tensors")
-            self.guard = torch.cuda.stream(stream)
-        elif torch.cuda.current_device() != device.index:
-            self.guard = torch.cuda.device(device)
+
+def _load():
+    global _t, _raw_stream
+    torch = _seer._torch()
+    # (the handle alone, where this torch offers it: the Stream object around it takes 1 to 3 us)
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+        (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _t = torch
+
+
+class _Here:
+    """No change of device or stream."""
 
     def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-        return _seer._torch().cuda.current_stream().cuda_stream
+        pass
 
     def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
+
+
+_HERE = _Here()
+
+
+def _on(dev, stream):
+    """What makes a call's device and stream current, so that memory which the call allocates belongs to the stream
+    that works on it."""
+    if stream is not None:
+        if stream.device.index != dev:
+            raise ValueError("the stream belongs to another device than the tensors")
+        return _t.cuda.stream(stream)
+    return _HERE if _t.cuda.current_device() == dev else _t.cuda.device(dev)
 
 
 def rope_freqs(rot_dim: int, theta: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
@@ -134,56 +146,66 @@ def rope_freqs(rot_dim: int, theta: float = 10000.0, *, scaling: str = "none", f
     return torch.tensor(f, dtype=torch.float64, device=device), scale
 
 
-def _token_strides(t, packed):
-    """(batch, head, token) strides of [B, H, S, D], or of packed [T, H, D] as one batch entry."""
-    st = t.stride()
-    return (0, st[1], st[0]) if packed else st[:3]
+_ZERO3 = (0, 0, 0)
 
 
 def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream, grad):
-    torch = _seer._torch()
-    packed = q.dim() == 3
-    if q.dim() not in (3, 4):
+    if _t is None:
+        _load()
+    shape = q.shape
+    if len(shape) == 4:
+        batch, heads, seq, dim = shape
+    elif len(shape) == 3:  # packed: one batch entry
+        (seq, heads, dim), batch = shape, 1
+    else:
         raise ValueError("q must be [batch, heads, seq, head_dim] or packed [tokens, heads, head_dim]")
     if inv_freq is None:
         raise ValueError("inv_freq is required")
-    qo, ko = out if out is not None else (None, None)
+    packed, kv = len(shape) == 3, 0
     if k is not None:
-        want = q.shape[:1] + k.shape[1:2] + q.shape[2:]
-        if k.dim() != q.dim() or k.shape != want:
+        ks = k.shape
+        if len(ks) != len(shape) or ks[0] != shape[0] or ks[2:] != shape[2:]:
             raise ValueError("k must be shaped like q, but for the heads")
-    for name, o, x in (("q", qo, q), ("k", ko, k)):
-        if o is not None and (x is None or o.shape != x.shape):
-            raise ValueError(f"the output of {name} must be shaped like it")
-    if out is not None and (qo is None or (ko is None) != (k is None)):
-        raise ValueError("out must hold an output for each input")
-    named = [(name, x) for name, x in (("q", q), ("k", k), ("out of q", qo), ("out of k", ko)) if x is not None]
-    device = _check_tensors(named, q.dtype)
-    if packed:
-        (seq, heads, dim), batch = q.shape, 1
-    else:
-        batch, heads, seq, dim = q.shape
-    pos_stride = 0
+        kv = ks[1]
+    qo, ko = (None, None) if out is None else out
+    if out is not None:
+        if qo is None or (ko is None) != (k is None):
+            raise ValueError("out must hold an output for each input")
+        if qo.shape != shape or (k is not None and ko.shape != k.shape):
+            raise ValueError("an output must be shaped like its input")
+    dev, dtype = q.get_device(), q.dtype
+    if dev < 0 or any(t is not None and (t.get_device() != dev or t.dtype is not dtype or t.stride(-1) != 1)
+                      for t in (q, k, qo, ko)):
+        _refuse_tensors(dtype, q=q, k=k, out_q=qo, out_k=ko)
+    pos_stride, pos = 0, None
     if positions is not None:
-        _check_ints("positions", positions, device, (1,) if packed else (1, 2))
-        if positions.shape[-1] != seq or (positions.dim() == 2 and positions.shape[0] != batch):
-            raise ValueError("positions must be [batch, seq] or [seq] (one for all), [tokens] of a packed batch")
-        if positions.dim() == 2:
+        _check_int("positions", positions, dev)
+        n = positions.shape
+        if n[-1] != seq or positions.stride(-1) != 1 and seq > 1 or not (
+                len(n) == 1 or len(n) == 2 and n[0] == batch and not packed):
+            raise ValueError("positions must be [batch, seq] or [seq] (one for all), [tokens] of a packed batch, with unit "
+                             "last stride")
+        if len(n) == 2:
             pos_stride = positions.stride(0)
-    params = _rope_arg(inv_freq, interleaved, rope_scale, device)
-    code, kv, zero = _seer._dtype_code(q), 0 if k is None else k.shape[1], (0, 0, 0)
-    with _On(device, stream) as raw:
+        pos = positions.data_ptr()
+    params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
+    code = _seer._dtype_code(q)
+    with _on(dev, stream):
         if out is None:
-            qo = torch.empty_like(q)
-            ko = None if k is None else torch.empty_like(k)
+            qo = _t.empty_like(q)
+            if k is not None:
+                ko = _t.empty_like(k)
         if q.numel() == 0:
             return qo, ko
-        desc = _ROPE_DESC.pack(batch, heads, kv, seq, dim, code, *_token_strides(q, packed),
-                               *(zero if k is None else _token_strides(k, packed)), *_token_strides(qo, packed),
-                               *(zero if k is None else _token_strides(ko, packed)), pos_stride)
-        st = _seer.lib().seer_rope(desc, params, q.data_ptr(), _seer._ptr(k), qo.data_ptr(), _seer._ptr(ko),
-                                   _seer._ptr(positions), int(start), grad, raw)
-    _seer._check(st, "seer_rope")
+        st = [t.stride() if t is not None else _ZERO3 for t in (q, k, qo, ko)]
+        if packed:
+            st = [(0, x[1], x[0]) for x in st]
+        a, b, c, d = st
+        desc = _ROPE_DESC.pack(batch, heads, kv, seq, dim, code, *a[:3], *b[:3], *c[:3], *d[:3], pos_stride)
+        status = _seer.lib().seer_rope(desc, params, q.data_ptr(), None if k is None else k.data_ptr(), qo.data_ptr(),
+                                       None if k is None else ko.data_ptr(), pos, start, grad, _raw_stream(dev))
+    if status:
+        _seer._check(status, "seer_rope")
     return qo, ko
 
 
@@ -210,30 +232,34 @@ def alloc_kv_cache(num_pages: int, page_size: int, heads_kv: int, head_dim: int,
     return tuple(torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
 
 
-def _check_cache(kc, vc, table, device, heads, dim):
-    if kc.dim() != 4 or vc.shape != kc.shape or kc.shape[3] != dim or (heads is not None and kc.shape[1] != heads):
+def _check_cache(kc, vc, table, dev, heads, dim):
+    shape = kc.shape
+    if len(shape) != 4 or vc.shape != shape or shape[3] != dim or (heads is not None and shape[1] != heads):
         raise ValueError("the caches must be [pages, heads_kv, page_size, head_dim], both alike")
-    _check_ints("table", table, device, (2,))
+    _check_int("table", table, dev)
+    if table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1):
+        raise ValueError("table must be [rows, pages] with unit last stride")
 
 
 def _tokens_of(x, name):
-    """(batch, heads, tokens, dim), strides of [B, H, S, D] or [B, H, D]."""
-    if x.dim() == 4:
-        return x.shape, x.stride()[:3]
-    if x.dim() == 3:
-        b, h, d = x.shape
-        return (b, h, 1, d), (x.stride(0), x.stride(1), 0)
+    """(batch, heads, tokens, dim) and strides of [B, H, S, D] or [B, H, D]."""
+    shape, st = x.shape, x.stride()
+    if len(shape) == 4:
+        return shape, st[:3]
+    if len(shape) == 3:
+        return (shape[0], shape[1], 1, shape[2]), (st[0], st[1], 0)
     raise ValueError(f"{name} must be [batch, heads, tokens, head_dim] or [batch, heads, head_dim]")
 
 
-def _per_token(name, t, device, batch, tokens):
+def _per_token(name, t, dev, batch, tokens):
     """Batch stride of int32 [batch, tokens], or [batch] where there is one token."""
-    _check_ints(name, t, device, (1, 2))
-    if tuple(t.shape) == (batch, tokens):
-        return t.stride(0)
-    if t.dim() == 1 and tokens == 1 and t.shape[0] == batch:
-        return t.stride(0)
-    raise ValueError(f"{name} must be [{batch}, {tokens}]")
+    _check_int(name, t, dev)
+    shape, st = t.shape, t.stride()
+    if len(shape) == 2 and shape[0] == batch and shape[1] == tokens and (st[1] == 1 or tokens == 1):
+        return st[0]
+    if len(shape) == 1 and tokens == 1 and shape[0] == batch:
+        return st[0]
+    raise ValueError(f"{name} must be [{batch}, {tokens}] with unit last stride")
 
 
 def kv_append(k, v, k_cache, v_cache, table, positions, *, rows=None, inv_freq=None, interleaved: bool = False,
@@ -242,39 +268,52 @@ def kv_append(k, v, k_cache, v_cache, table, positions, *, rows=None, inv_freq=N
     when inv_freq is given.  k, v: [B, Hkv, S, D], or [T, Hkv, D]; positions: int32 [B, S] ([T]); rows: the table row of
     each token, shaped like positions (None: row b of [B, Hkv, S, D], row t of [T, Hkv, D]).  Tokens with a negative
     position or row are padding."""
+    if _t is None:
+        _load()
     if v.shape != k.shape:
         raise ValueError("k and v must be shaped alike")
     (batch, heads, tokens, dim), ks = _tokens_of(k, "k")
     vs = _tokens_of(v, "v")[1]
-    device = _check_tensors((("k", k), ("v", v), ("k_cache", k_cache), ("v_cache", v_cache)), k.dtype)
-    _check_cache(k_cache, v_cache, table, device, heads, dim)
-    pos_stride = _per_token("positions", positions, device, batch, tokens)
-    if rows is not None and _per_token("rows", rows, device, batch, tokens) != pos_stride:
+    dev, dtype = k.get_device(), k.dtype
+    if dev < 0 or any(t.get_device() != dev or t.dtype is not dtype or t.stride(-1) != 1
+                      for t in (k, v, k_cache, v_cache)):
+        _refuse_tensors(dtype, k=k, v=v, k_cache=k_cache, v_cache=v_cache)
+    _check_cache(k_cache, v_cache, table, dev, heads, dim)
+    pos_stride = _per_token("positions", positions, dev, batch, tokens)
+    if rows is not None and _per_token("rows", rows, dev, batch, tokens) != pos_stride and batch > 1:
         raise ValueError("rows must be laid out like positions")
-    params = _rope_arg(inv_freq, interleaved, rope_scale, device)
+    params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
+    code = _seer._dtype_code(k)
     if k.numel() == 0:
         return
-    desc = _CACHE_DESC.pack(batch, tokens, heads, dim, _seer._dtype_code(k), k_cache.shape[2], k_cache.shape[0],
-                            table.shape[0], table.shape[1], 0, *ks, *vs, *k_cache.stride()[:3], *v_cache.stride()[:3],
-                            table.stride(0), pos_stride)
-    with _On(device, stream) as raw:
-        st = _seer.lib().seer_kv_append(desc, params, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(),
-                                        v_cache.data_ptr(), table.data_ptr(), positions.data_ptr(), _seer._ptr(rows),
-                                        raw)
-    _seer._check(st, "seer_kv_append")
+    pages, _, page_size, _ = k_cache.shape
+    n_rows, max_pages = table.shape
+    desc = _CACHE_DESC.pack(batch, tokens, heads, dim, code, page_size, pages, n_rows, max_pages, 0, *ks, *vs,
+                            *k_cache.stride()[:3], *v_cache.stride()[:3], table.stride(0), pos_stride)
+    with _on(dev, stream):
+        status = _seer.lib().seer_kv_append(desc, params, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(),
+                                            v_cache.data_ptr(), table.data_ptr(), positions.data_ptr(),
+                                            None if rows is None else rows.data_ptr(), _raw_stream(dev))
+    if status:
+        _seer._check(status, "seer_kv_append")
 
 
-def _paged_desc(q, o, k_cache, v_cache, table, pos_stride):
-    (batch, heads, tokens, dim), qs = _tokens_of(q, "q")
-    return _CACHE_DESC.pack(batch, heads, k_cache.shape[1], tokens, dim, _seer._dtype_code(q), k_cache.shape[2],
-                            k_cache.shape[0], table.shape[1], 0, *qs, *_tokens_of(o, "out")[1],
+def _paged_desc(shape, qs, os_, code, k_cache, v_cache, table, pos_stride):
+    pages, heads_kv, page_size, _ = k_cache.shape
+    batch, heads, tokens, dim = shape
+    return _CACHE_DESC.pack(batch, heads, heads_kv, tokens, dim, code, page_size, pages, table.shape[1], 0, *qs, *os_,
                             *k_cache.stride()[:3], *v_cache.stride()[:3], table.stride(0), pos_stride)
 
 
 def paged_attn_workspace_bytes(q, k_cache, v_cache, table) -> int:
     """Workspace of paged_attn for these shapes (0: the call would refuse them)."""
-    return _seer.lib().seer_paged_attn_workspace_bytes(_paged_desc(q, _seer._torch().empty_like(q), k_cache, v_cache,
-                                                                   table, 0))
+    if _t is None:
+        _load()
+    shape, qs = _tokens_of(q, "q")
+    _, heads, tokens, dim = shape
+    desc = _paged_desc(shape, qs, (heads * tokens * dim, tokens * dim, dim), _seer._dtype_code(q), k_cache, v_cache, table,
+                       0)
+    return _seer.lib().seer_paged_attn_workspace_bytes(desc)
 
 
 def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interleaved: bool = False,
@@ -284,35 +323,42 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
     each sequence; positions: int32 [B, S] ([B]): a token sees the keys up to its own position, none where that is
     negative.  inv_freq: q is rotated at its position first.  A workspace given by the caller must not serve two calls
     that may run at the same time.  Returns (O, LSE [B, Hq, S] ([B, Hq]) or None)."""
-    torch = _seer._torch()
-    (batch, heads, tokens, dim), _ = _tokens_of(q, "q")
-    if out is not None and out.shape != q.shape:
-        raise ValueError("out must be shaped like q")
-    named = [("q", q), ("k_cache", k_cache), ("v_cache", v_cache)] + ([] if out is None else [("out", out)])
-    device = _check_tensors(named, q.dtype)
-    _check_cache(k_cache, v_cache, table, device, None, dim)
+    if _t is None:
+        _load()
+    shape, qs = _tokens_of(q, "q")
+    batch, _, tokens, dim = shape
+    dev, dtype = q.get_device(), q.dtype
+    if dev < 0 or any(t is not None and (t.get_device() != dev or t.dtype is not dtype or t.stride(-1) != 1)
+                      for t in (q, k_cache, v_cache, out)):
+        _refuse_tensors(dtype, q=q, k_cache=k_cache, v_cache=v_cache, out=out)
+    _check_cache(k_cache, v_cache, table, dev, None, dim)
     if table.shape[0] != batch:
         raise ValueError("table must have a row for each batch entry")
-    pos_stride = _per_token("positions", positions, device, batch, tokens)
-    params = _rope_arg(inv_freq, interleaved, rope_scale, device)
-    if lse is not None and (lse.shape != q.shape[:-1] or lse.dtype != torch.float32 or lse.device != device or
+    if out is not None and out.shape != q.shape:
+        raise ValueError("out must be shaped like q")
+    pos_stride = _per_token("positions", positions, dev, batch, tokens)
+    params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
+    code = _seer._dtype_code(q)
+    if lse is not None and (lse.shape != q.shape[:-1] or lse.dtype is not _t.float32 or lse.get_device() != dev or
                             not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [batch, heads, tokens] on the GPU of the other tensors")
-    if workspace is not None and (workspace.device != device or not workspace.is_contiguous()):
+    if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("workspace must be contiguous and on the GPU of the other tensors")
-    L = _seer.lib()
-    with _On(device, stream) as raw:
-        o = torch.empty_like(q) if out is None else out
+    lib = _seer.lib()
+    with _on(dev, stream):
+        o = _t.empty_like(q) if out is None else out
         if lse is None and want_lse:
-            lse = torch.empty(q.shape[:-1], dtype=torch.float32, device=device)
+            lse = _t.empty(q.shape[:-1], dtype=_t.float32, device=q.device)
         if q.numel() == 0:
             return o, lse
-        desc = _paged_desc(q, o, k_cache, v_cache, table, pos_stride)
+        desc = _paged_desc(shape, qs, _tokens_of(o, "out")[1], code, k_cache, v_cache, table, pos_stride)
         if workspace is None:
-            need = L.seer_paged_attn_workspace_bytes(desc)
-            workspace = torch.empty(max(need, 1), dtype=torch.uint8, device=device)
-        st = L.seer_paged_attn(desc, params, float(sm_scale), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                               table.data_ptr(), positions.data_ptr(), o.data_ptr(), _seer._ptr(lse),
-                               workspace.data_ptr(), workspace.numel() * workspace.element_size(), raw)
-    _seer._check(st, "seer_paged_attn")
+            need = lib.seer_paged_attn_workspace_bytes(desc)
+            workspace = _t.empty(need or 1, dtype=_t.uint8, device=q.device)
+        status = lib.seer_paged_attn(desc, params, sm_scale, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                                     table.data_ptr(), positions.data_ptr(), o.data_ptr(),
+                                     None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    if status:
+        _seer._check(status, "seer_paged_attn")
     return o, lse
