@@ -36,7 +36,6 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWorkers = 512;   // workgroups at most: two for each CU
-constexpr int kRowCost = 1;     // a row's beginning and end, in units: what it weighs beside its units
 constexpr int kWholeKeys = 512; // caches of at most this many tokens a sequence are never split
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -154,6 +153,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NA = D / 16;          // accumulators of a column tile
   constexpr int ROWS = 16 * NT;
+  // A row's beginning and end, in units: what it weighs beside its units (64 sequences of 200 to 16000 tokens: 189 us
+  // without, 180 with 1, 181 with 2; four drafted tokens on two column tiles: 61.3, 56.0, 55.0)
+  constexpr int kRowCost = NT;
   constexpr int OSTR = D + 4;
   constexpr int QJ = BF ? D / 32 : D / 16;
   // the operand Q^T as the lanes read it, then the wavefronts' results
@@ -664,15 +666,17 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   }
 }
 
-// Rows whose keys several workgroups shared: their partial results, in the order of the keys.
-// A workgroup joins JR rows of an item; a thread sums 4 features over the parts grp, grp + GRP, ..
-constexpr int kJoinThreads = 256, kJoinRows = 4;
-template <typename T, int D>
+// Rows whose keys several workgroups shared: their partial results, in the order of the keys.  A workgroup joins JR
+// rows of an item, a wavefront forming the weights of a row (or part of one: all four then form the same); a thread sums
+// 4 features over the parts grp, grp + GRP, ..  Four rows a workgroup keep a large batch's launch short, one row leaves
+// fewer parts to each thread where the call has few rows (a token after 131072 tokens, 32 heads of 64 parts: 7.3 -> 3.9 us).
+constexpr int kJoinThreads = 256;
+template <typename T, int D, int JR>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka, int rows_block) {
-  constexpr int V4 = D / 4, GRP = kJoinThreads / (V4 * kJoinRows), AHEAD = 8;
-  __shared__ float sW[kJoinRows][kWorkers];
-  __shared__ float2 sT[kJoinRows];
-  __shared__ __attribute__((aligned(16))) float sO[GRP][kJoinRows][D];
+  constexpr int V4 = D / 4, GRP = kJoinThreads / (V4 * JR), AHEAD = 8, OWN = kWorkers / kWave;
+  __shared__ float sW[JR][kWorkers];
+  __shared__ float2 sT[JR];
+  __shared__ __attribute__((aligned(16))) float sO[GRP][JR][D];
   const PagedArgs& a = ka.a;
   const int64_t at = blockIdx.x;
   const int2 rec = ka.record[at];
@@ -687,29 +691,34 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka,
   const float c = ka.scale_log2;
 
   // the first parts are on their way while the weights are formed
-  const int d = tid % V4 * 4, jr = tid / V4 % kJoinRows, grp = tid / (V4 * kJoinRows);
-  const int rl = min((int)blockIdx.y * kJoinRows + jr, nrows - 1);
+  const int wrow = wave % JR;
+  const int row = min((int)blockIdx.y * JR + wrow, nrows - 1);
+  float2 ml[OWN];
+#pragma unroll
+  for (int i = 0; i < OWN; ++i)
+    if (i * kWave < parts) ml[i] = ka.part_ml[slot(min(lane + i * kWave, parts - 1), row)];
+  const int d = tid % V4 * 4, jr = tid / V4 % JR, grp = tid / (V4 * JR);
+  const int rl = min((int)blockIdx.y * JR + jr, nrows - 1);
   auto part = [&](int p) { return *(const f32x4*)(ka.part_o + slot(p, rl) * D + d); };
   f32x4 y[AHEAD];
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) y[i] = part(min(grp + i * GRP, parts - 1));
 
-  static_assert(kJoinRows == kJoinThreads / kWave, "a wavefront forms one row's weights");
-  {
-    const int row = min((int)blockIdx.y * kJoinRows + wave, nrows - 1);
-    float mx = -INFINITY;
-    for (int p = lane; p < parts; p += kWave) mx = fmaxf(mx, ka.part_ml[slot(p, row)].x);
-    mx = wave_max(mx);
-    float sum = 0.f;
-    for (int p = lane; p < parts; p += kWave) {
-      const float2 ml = ka.part_ml[slot(p, row)];
-      const float wgt = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml.x - mx) * c);
-      sW[wave][p] = wgt;
-      sum += wgt * ml.y;
+  float mx = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < OWN; ++i)
+    if (i * kWave < parts) mx = fmaxf(mx, ml[i].x);
+  mx = wave_max(mx);
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < OWN; ++i)
+    if (lane + i * kWave < parts) {
+      const float wgt = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - mx) * c);
+      if (wave < JR) sW[wrow][lane + i * kWave] = wgt;
+      sum += wgt * ml[i].y;
     }
-    sum = wave_sum(sum);
-    if (lane == 0) sT[wave] = make_float2(mx, sum);
-  }
+  sum = wave_sum(sum);
+  if (lane == 0 && wave < JR) sT[wrow] = make_float2(mx, sum);
   __syncthreads();
 
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -720,10 +729,11 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka,
   for (int p = grp + AHEAD * GRP; p < parts; p += GRP) o += sW[jr][p] * part(p);
   *(f32x4*)&sO[grp][jr][d] = o;
   __syncthreads();
-  if (grp != 0 || (int)blockIdx.y * kJoinRows + jr >= nrows) return;
+  if (grp != 0 || (int)blockIdx.y * JR + jr >= nrows) return;
 #pragma unroll
   for (int i = 1; i < GRP; ++i) o += *(const f32x4*)&sO[i][jr][d];
-  const float mx = sT[jr].x, sum = sT[jr].y;
+  mx = sT[jr].x;
+  sum = sT[jr].y;
   const int r = rb * rows_block + rl, t = r / ka.group, hq = h * ka.group + (r - t * ka.group);
   const bool none = sum == 0.f || a.positions[b * a.pos_stride + t] < 0;
   T* out = (T*)a.o + b * a.osb + hq * a.osh + t * a.oss + d;
@@ -772,8 +782,12 @@ hipError_t launch_typed(const KernelArgs& k, int nt, dim3 grid, hipStream_t s) {
     e = nt == 2 ? launch<T, D, 2, 1>(k, grid, s) : launch<T, D, 1, 1>(k, grid, s);
   }
   if (e != hipSuccess || !k.join) return e;
-  const int64_t rows = (int64_t)k.a.batch * k.a.heads_kv * k.row_blocks;
-  paged_join_kernel<T, D><<<dim3((unsigned)rows, (unsigned)((std::min(k.rows, 16 * nt) + kJoinRows - 1) / kJoinRows)), kJoinThreads, 0, s>>>(k, 16 * nt);
+  const int64_t all = (int64_t)k.a.batch * k.a.heads_kv * k.row_blocks;
+  const int rows = std::min(k.rows, 16 * nt);
+  if (all * rows <= 2 * kWorkers)
+    paged_join_kernel<T, D, 1><<<dim3((unsigned)all, (unsigned)rows), kJoinThreads, 0, s>>>(k, 16 * nt);
+  else
+    paged_join_kernel<T, D, 4><<<dim3((unsigned)all, (unsigned)((rows + 3) / 4)), kJoinThreads, 0, s>>>(k, 16 * nt);
   return hipGetLastError();
 }
 
@@ -799,9 +813,9 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   int64_t unit = step;
   k.join = k.capacity > kWholeKeys;
   if (!k.join) unit = (k.capacity + step - 1) / step * step;
-  // (counts of units stay below 2^31)
+  // (weights stay below 2^31)
   auto units = [&]() { return (k.capacity + unit - 1) / unit; };
-  while ((units() + kRowCost) * std::max((int64_t)a.batch, items) > INT32_MAX / 2 && unit < (1 << 29)) unit *= 2;
+  while ((units() + 2) * std::max((int64_t)a.batch, items) > INT32_MAX / 2 && unit < (1 << 29)) unit *= 2;
   k.unit = (int)unit;
   k.scale_log2 = a.scale * kLog2e;
   char* ws = (char*)a.workspace;

@@ -84,27 +84,14 @@ def _load():
     _t = torch
 
 
-class _Here:
-    """No change of device or stream."""
-
-    def __enter__(self):
-        pass
-
-    def __exit__(self, *exc):
-        pass
-
-
-_HERE = _Here()
-
-
-def _on(dev, stream):
-    """What makes a call's device and stream current, so that memory which the call allocates belongs to the stream
-    that works on it."""
-    if stream is not None:
-        if stream.device.index != dev:
-            raise ValueError("the stream belongs to another device than the tensors")
-        return _t.cuda.stream(stream)
-    return _HERE if _t.cuda.current_device() == dev else _t.cuda.device(dev)
+def _elsewhere(dev, stream):
+    """A context that makes the stream, or else the device, current: memory which the call allocates then belongs to the
+    stream that works on it."""
+    if stream is None:
+        return _t.cuda.device(dev)
+    if stream.device.index != dev:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return _t.cuda.stream(stream)
 
 
 def rope_freqs(rot_dim: int, theta: float = 10000.0, *, scaling: str = "none", factor: float = 1.0,
@@ -146,7 +133,7 @@ def rope_freqs(rot_dim: int, theta: float = 10000.0, *, scaling: str = "none", f
     return torch.tensor(f, dtype=torch.float64, device=device), scale
 
 
-_ZERO3 = (0, 0, 0)
+_ZERO = (0, 0, 0)
 
 
 def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream, grad):
@@ -163,20 +150,24 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
         raise ValueError("inv_freq is required")
     packed, kv = len(shape) == 3, 0
     if k is not None:
-        ks = k.shape
-        if len(ks) != len(shape) or ks[0] != shape[0] or ks[2:] != shape[2:]:
+        n = k.shape
+        if len(n) != len(shape) or n[0] != shape[0] or n[2:] != shape[2:]:
             raise ValueError("k must be shaped like q, but for the heads")
-        kv = ks[1]
+        kv = n[1]
     qo, ko = (None, None) if out is None else out
     if out is not None:
         if qo is None or (ko is None) != (k is None):
             raise ValueError("out must hold an output for each input")
         if qo.shape != shape or (k is not None and ko.shape != k.shape):
             raise ValueError("an output must be shaped like its input")
-    dev, dtype = q.get_device(), q.dtype
-    if dev < 0 or any(t is not None and (t.get_device() != dev or t.dtype is not dtype or t.stride(-1) != 1)
-                      for t in (q, k, qo, ko)):
+    dev, dtype, qs = q.get_device(), q.dtype, q.stride()
+    ks = _ZERO if k is None else k.stride()
+    if (dev < 0 or qs[-1] != 1 or out is not None
+            or k is not None and (k.get_device() != dev or k.dtype is not dtype or ks[-1] != 1)):
         _refuse_tensors(dtype, q=q, k=k, out_q=qo, out_k=ko)
+    if stream is not None or _t.cuda.current_device() != dev:
+        with _elsewhere(dev, stream):
+            return _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, None, grad)
     pos_stride, pos = 0, None
     if positions is not None:
         _check_int("positions", positions, dev)
@@ -190,20 +181,18 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
         pos = positions.data_ptr()
     params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
     code = _seer._dtype_code(q)
-    with _on(dev, stream):
-        if out is None:
-            qo = _t.empty_like(q)
-            if k is not None:
-                ko = _t.empty_like(k)
-        if q.numel() == 0:
-            return qo, ko
-        st = [t.stride() if t is not None else _ZERO3 for t in (q, k, qo, ko)]
-        if packed:
-            st = [(0, x[1], x[0]) for x in st]
-        a, b, c, d = st
-        desc = _ROPE_DESC.pack(batch, heads, kv, seq, dim, code, *a[:3], *b[:3], *c[:3], *d[:3], pos_stride)
-        status = _seer.lib().seer_rope(desc, params, q.data_ptr(), None if k is None else k.data_ptr(), qo.data_ptr(),
-                                       None if k is None else ko.data_ptr(), pos, start, grad, _raw_stream(dev))
+    if out is None:
+        qo = _t.empty_like(q)
+        if k is not None:
+            ko = _t.empty_like(k)
+    if q.numel() == 0:
+        return qo, ko
+    os_, kos = qo.stride(), _ZERO if k is None else ko.stride()
+    if packed:
+        qs, ks, os_, kos = ((0, x[1], x[0]) for x in (qs, ks, os_, kos))
+    desc = _ROPE_DESC.pack(batch, heads, kv, seq, dim, code, *qs[:3], *ks[:3], *os_[:3], *kos[:3], pos_stride)
+    status = _seer.lib().seer_rope(desc, params, q.data_ptr(), None if k is None else k.data_ptr(), qo.data_ptr(),
+                                   None if k is None else ko.data_ptr(), pos, start, grad, _raw_stream(dev))
     if status:
         _seer._check(status, "seer_rope")
     return qo, ko
@@ -274,10 +263,15 @@ def kv_append(k, v, k_cache, v_cache, table, positions, *, rows=None, inv_freq=N
         raise ValueError("k and v must be shaped alike")
     (batch, heads, tokens, dim), ks = _tokens_of(k, "k")
     vs = _tokens_of(v, "v")[1]
-    dev, dtype = k.get_device(), k.dtype
-    if dev < 0 or any(t.get_device() != dev or t.dtype is not dtype or t.stride(-1) != 1
-                      for t in (k, v, k_cache, v_cache)):
+    dev, dtype, kcs, vcs = k.get_device(), k.dtype, k_cache.stride(), v_cache.stride()
+    if (dev < 0 or v.get_device() != dev or k_cache.get_device() != dev or v_cache.get_device() != dev
+            or v.dtype is not dtype or k_cache.dtype is not dtype or v_cache.dtype is not dtype
+            or k.stride(-1) != 1 or v.stride(-1) != 1 or kcs[-1] != 1 or vcs[-1] != 1):
         _refuse_tensors(dtype, k=k, v=v, k_cache=k_cache, v_cache=v_cache)
+    if stream is not None or _t.cuda.current_device() != dev:
+        with _elsewhere(dev, stream):
+            return kv_append(k, v, k_cache, v_cache, table, positions, rows=rows, inv_freq=inv_freq,
+                             interleaved=interleaved, rope_scale=rope_scale)
     _check_cache(k_cache, v_cache, table, dev, heads, dim)
     pos_stride = _per_token("positions", positions, dev, batch, tokens)
     if rows is not None and _per_token("rows", rows, dev, batch, tokens) != pos_stride and batch > 1:
@@ -289,11 +283,10 @@ def kv_append(k, v, k_cache, v_cache, table, positions, *, rows=None, inv_freq=N
     pages, _, page_size, _ = k_cache.shape
     n_rows, max_pages = table.shape
     desc = _CACHE_DESC.pack(batch, tokens, heads, dim, code, page_size, pages, n_rows, max_pages, 0, *ks, *vs,
-                            *k_cache.stride()[:3], *v_cache.stride()[:3], table.stride(0), pos_stride)
-    with _on(dev, stream):
-        status = _seer.lib().seer_kv_append(desc, params, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(),
-                                            v_cache.data_ptr(), table.data_ptr(), positions.data_ptr(),
-                                            None if rows is None else rows.data_ptr(), _raw_stream(dev))
+                            *kcs[:3], *vcs[:3], table.stride(0), pos_stride)
+    status = _seer.lib().seer_kv_append(desc, params, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                                        table.data_ptr(), positions.data_ptr(), None if rows is None else rows.data_ptr(),
+                                        _raw_stream(dev))
     if status:
         _seer._check(status, "seer_kv_append")
 
@@ -328,9 +321,15 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
     shape, qs = _tokens_of(q, "q")
     batch, _, tokens, dim = shape
     dev, dtype = q.get_device(), q.dtype
-    if dev < 0 or any(t is not None and (t.get_device() != dev or t.dtype is not dtype or t.stride(-1) != 1)
-                      for t in (q, k_cache, v_cache, out)):
+    if (dev < 0 or k_cache.get_device() != dev or v_cache.get_device() != dev or k_cache.dtype is not dtype
+            or v_cache.dtype is not dtype or q.stride(-1) != 1 or k_cache.stride(-1) != 1 or v_cache.stride(-1) != 1
+            or out is not None):
         _refuse_tensors(dtype, q=q, k_cache=k_cache, v_cache=v_cache, out=out)
+    if stream is not None or _t.cuda.current_device() != dev:
+        with _elsewhere(dev, stream):
+            return paged_attn(q, k_cache, v_cache, table, positions, inv_freq=inv_freq, interleaved=interleaved,
+                              rope_scale=rope_scale, sm_scale=sm_scale, out=out, lse=lse, want_lse=want_lse,
+                              workspace=workspace)
     _check_cache(k_cache, v_cache, table, dev, None, dim)
     if table.shape[0] != batch:
         raise ValueError("table must have a row for each batch entry")
@@ -345,20 +344,19 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("workspace must be contiguous and on the GPU of the other tensors")
     lib = _seer.lib()
-    with _on(dev, stream):
-        o = _t.empty_like(q) if out is None else out
-        if lse is None and want_lse:
-            lse = _t.empty(q.shape[:-1], dtype=_t.float32, device=q.device)
-        if q.numel() == 0:
-            return o, lse
-        desc = _paged_desc(shape, qs, _tokens_of(o, "out")[1], code, k_cache, v_cache, table, pos_stride)
-        if workspace is None:
-            need = lib.seer_paged_attn_workspace_bytes(desc)
-            workspace = _t.empty(need or 1, dtype=_t.uint8, device=q.device)
-        status = lib.seer_paged_attn(desc, params, sm_scale, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                     table.data_ptr(), positions.data_ptr(), o.data_ptr(),
-                                     None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    o = _t.empty_like(q) if out is None else out
+    if lse is None and want_lse:
+        lse = _t.empty(q.shape[:-1], dtype=_t.float32, device=q.device)
+    if q.numel() == 0:
+        return o, lse
+    desc = _paged_desc(shape, qs, _tokens_of(o, "out")[1], code, k_cache, v_cache, table, pos_stride)
+    if workspace is None:
+        need = lib.seer_paged_attn_workspace_bytes(desc)
+        workspace = _t.empty(need or 1, dtype=_t.uint8, device=q.device)
+    status = lib.seer_paged_attn(desc, params, sm_scale, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                                 table.data_ptr(), positions.data_ptr(), o.data_ptr(),
+                                 None if lse is None else lse.data_ptr(), workspace.data_ptr(),
+                                 workspace.numel() * workspace.element_size(), _raw_stream(dev))
     if status:
         _seer._check(status, "seer_paged_attn")
     return o, lse
