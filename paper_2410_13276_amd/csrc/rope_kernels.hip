@@ -1,11 +1,10 @@
 // rope_kernels.hip -- rotary positions of Q and K (seer_rope) and the append of new
 // keys and values to a paged cache (seer_kv_append).
 //
-// Both move memory: two reads or writes of every element and some 20 operations on
-// it.  A thread owns 16 planes' halves of one token (two 16-byte pieces of a head in
-// bf16, 8 planes in fp32: VEC planes each), forms their cosines and sines once and
-// walks over heads with them, so that the angles (about 30 instructions a plane) are shared by
-// up to HB heads and every access is 16 bytes.  No table of cosines is read: the angle is an
+// Both move memory: a read and a write of every element, and some 10 operations on
+// it.  A thread owns two 16-byte pieces of one token's heads (8 planes in bf16, 4 in fp32), forms their
+// cosines and sines once and walks over up to 8 heads with them, so that the angles (about 30
+// instructions a plane) are shared and every access is 16 bytes.  No table of cosines is read: the angle is an
 // integer product of the position and the plane's turn rate (decode.h).
 #include <algorithm>
 
@@ -57,41 +56,55 @@ struct Vec<float> {
   }
 };
 
-// A thread's two 16-byte pieces of a head: where they begin, and whether they turn.
-template <typename T>
+// A thread's two 16-byte pieces of a head: where they begin, their first planes and whether they turn.  The
+// first pieces of a token's threads stand side by side, and so do the second ones, so that an access of a
+// wavefront covers whole lines (two pieces side by side in each thread: 153 us for 32768 tokens where this
+// takes 126, and 205 with the stores below).
 struct Pieces {
-  int lo, hi;
-  bool turn;
+  int lo, hi;         // elements
+  int plane[2];       // adjacent planes: each piece holds its own; half layout: the same ones, half of them in each
+  bool turn[2];
 };
-template <typename T, int D, bool INTER>
-__device__ __forceinline__ Pieces<T> pieces(int c, int rot) {
-  constexpr int N = Vec<T>::N;
-  Pieces<T> p;
-  p.turn = c < rot / (2 * N);
-  if (p.turn && !INTER) {
+template <int N, int D, bool INTER>
+__device__ __forceinline__ Pieces pieces(int c, int rot) {
+  Pieces p;
+  const int turning = INTER ? 0 : rot / (2 * N);  // threads that hold both halves of N planes
+  if (c < turning) {
     p.lo = c * N;
     p.hi = rot / 2 + c * N;
-  } else {  // adjacent planes, or elements past rot: 2N elements in a row
-    p.lo = 2 * c * N;
-    p.hi = p.lo + N;
+    p.plane[0] = p.plane[1] = c * N;
+    p.turn[0] = p.turn[1] = true;
+  } else {
+    const int first = INTER ? 0 : rot;
+    p.lo = first + (c - turning) * N;
+    p.hi = p.lo + (D - first) / 2;
+    p.plane[0] = p.lo / 2;
+    p.plane[1] = p.hi / 2;
+    p.turn[0] = INTER && p.lo < rot;
+    p.turn[1] = INTER && p.hi < rot;
   }
   return p;
 }
 
-// The factors of the thread's N planes at position pos (scale in both).
-template <int N>
-__device__ __forceinline__ void factors(const RopeView& r, int c, int pos, bool grad, float (&cs)[N], float (&sn)[N]) {
+// The factors of the thread's N planes at position pos (scale in both): N of the half layout, N / 2 of each piece
+// of the other.
+template <int N, bool INTER>
+__device__ __forceinline__ void factors(const RopeView& r, const Pieces& p, int pos, bool grad, float (&cs)[N],
+                                        float (&sn)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) {
+    const int h = INTER ? i / (N / 2) : 0;
+    if (!p.turn[h]) continue;
     float co, si;
-    turn_cos_sin(turn_rate(r.freq[c * N + i]), pos, co, si);
+    turn_cos_sin(turn_rate(r.freq[p.plane[h] + (INTER ? i % (N / 2) : i)]), pos, co, si);
     cs[i] = co * r.scale;
     sn[i] = si * (grad ? -r.scale : r.scale);
   }
 }
 
 template <typename T, bool INTER>
-__device__ __forceinline__ void turn(u32x4& lo, u32x4& hi, const float (&cs)[Vec<T>::N], const float (&sn)[Vec<T>::N]) {
+__device__ __forceinline__ void turn(const Pieces& p, u32x4& lo, u32x4& hi, const float (&cs)[Vec<T>::N],
+                                     const float (&sn)[Vec<T>::N]) {
   constexpr int N = Vec<T>::N;
   float a[N], b[N], x[N], y[N];
   Vec<T>::unpack(lo, a);
@@ -111,22 +124,32 @@ __device__ __forceinline__ void turn(u32x4& lo, u32x4& hi, const float (&cs)[Vec
       y[i] = a[i] * sn[i] + b[i] * cs[i];
     }
   }
-  lo = Vec<T>::pack(x);
-  hi = Vec<T>::pack(y);
+  if (p.turn[0]) lo = Vec<T>::pack(x);
+  if (p.turn[1]) hi = Vec<T>::pack(y);
 }
 
-template <typename T, int D, bool INTER>
+// Stores that do not stay in the L2 (PAST): what is written here is read by a later launch.  They pay where a
+// wavefront's store covers whole 64-byte runs (rope of 8192 tokens, 32 + 8 heads: 34.4 -> 27.1 us; 20 prompts of 25000 tokens
+// to the cache: 45.8 -> 40.8) and cost where it does not (heads of 128 of which 32 turn, in halves: 46.4 -> 59.5).
+template <bool PAST>
+__device__ __forceinline__ void store(void* p, const u32x4& v) {
+  if constexpr (PAST) __builtin_nontemporal_store(v, (u32x4*)p);
+  else *(u32x4*)p = v;
+}
+
+template <typename T, int D, bool INTER, bool PAST>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, FastDiv per_b, int hb) {
   constexpr int N = Vec<T>::N, TPT = D / (2 * N), TOK = kThreads / TPT;
   const int t = (int)blockIdx.x * TOK + (int)threadIdx.x / TPT;  // tokens of all batch entries in a row
   const int c = threadIdx.x % TPT;
   if (t >= a.batch * a.seq_len) return;
   const int b = fast_quot(per_b, t), s = t - b * a.seq_len;
-  const Pieces<T> p = pieces<T, D, INTER>(c, a.rope.rot);
+  const Pieces p = pieces<N, D, INTER>(c, a.rope.rot);
   float cs[N], sn[N];
-  if (p.turn) {
+  const bool turns = p.turn[0] || p.turn[1];
+  if (turns) {
     const int pos = a.positions ? a.positions[b * a.pos_stride + s] : a.start + s;
-    factors<N>(a.rope, c, pos, a.grad, cs, sn);
+    factors<N, INTER>(a.rope, p, pos, a.grad, cs, sn);
   }
   const int heads = a.heads_q + a.heads_kv;
   const int h0 = blockIdx.y * hb, h1 = min(h0 + hb, heads);
@@ -144,15 +167,15 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(RotateArgs a, FastDiv 
     for (int i = 0; i < kAhead; ++i) {
       if (h + i >= h1) break;
       T* dst = h + i < a.heads_q ? at(a.qo, h + i) : at(a.ko, h + i - a.heads_q);
-      if (p.turn) turn<T, INTER>(lo[i], hi[i], cs, sn);
-      *(u32x4*)(dst + p.lo) = lo[i];
-      *(u32x4*)(dst + p.hi) = hi[i];
+      if (turns) turn<T, INTER>(p, lo[i], hi[i], cs, sn);
+      store<PAST>(dst + p.lo, lo[i]);
+      store<PAST>(dst + p.hi, hi[i]);
     }
   }
 }
 
 // A thread's planes of one token of every head of its share: K rotated, V copied.
-template <typename T, int D, bool INTER>
+template <typename T, int D, bool INTER, bool PAST>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, FastDiv per_b, int hb) {
   constexpr int N = Vec<T>::N, TPT = D / (2 * N), TOK = kThreads / TPT;
   const int t = (int)blockIdx.x * TOK + (int)threadIdx.x / TPT;  // tokens of all batch entries in a row
@@ -167,9 +190,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, FastDiv 
   const int page = a.table.ptr[row * a.table.stride + i];
   if (page < 0 || page >= a.table.num_pages) return;
   const int slot = pos - i * a.table.page.d;
-  const Pieces<T> p = pieces<T, D, INTER>(c, a.rope.rot);
+  const Pieces p = pieces<N, D, INTER>(c, a.rope.rot);
   float cs[N], sn[N];
-  if (p.turn) factors<N>(a.rope, c, pos, false, cs, sn);
+  const bool turns = p.turn[0] || p.turn[1];
+  if (turns) factors<N, INTER>(a.rope, p, pos, false, cs, sn);
   const int h0 = blockIdx.y * hb, h1 = min(h0 + hb, a.heads_kv);
   const T* k = (const T*)a.k.ptr + b * a.k.sb + s * a.k.ss;
   const T* v = (const T*)a.v.ptr + b * a.v.sb + s * a.v.ss;
@@ -189,18 +213,18 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, FastDiv 
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       if (h + j >= h1) break;
-      if (p.turn) turn<T, INTER>(klo[j], khi[j], cs, sn);
-      *(u32x4*)(kc + (h + j) * a.kc.sh + p.lo) = klo[j];
-      *(u32x4*)(kc + (h + j) * a.kc.sh + p.hi) = khi[j];
-      *(u32x4*)(vc + (h + j) * a.vc.sh + p.lo) = vlo[j];
-      *(u32x4*)(vc + (h + j) * a.vc.sh + p.hi) = vhi[j];
+      if (turns) turn<T, INTER>(p, klo[j], khi[j], cs, sn);
+      store<PAST>(kc + (h + j) * a.kc.sh + p.lo, klo[j]);
+      store<PAST>(kc + (h + j) * a.kc.sh + p.hi, khi[j]);
+      store<PAST>(vc + (h + j) * a.vc.sh + p.lo, vlo[j]);
+      store<PAST>(vc + (h + j) * a.vc.sh + p.hi, vhi[j]);
     }
   }
 }
 
-// Heads per workgroup: as many as leave the launch 2048 workgroups, 1 to 8.
-int head_share(int64_t tiles, int heads) {
-  int hb = 8;
+// Heads per workgroup: at most `most`, fewer where that leaves the launch less than 2048 workgroups.
+int head_share(int64_t tiles, int heads, int most) {
+  int hb = most;
   while (hb > 1 && tiles * ((heads + hb - 1) / hb) < 2048) hb /= 2;
   return hb;
 }
@@ -210,10 +234,14 @@ hipError_t rotate(const RotateArgs& a, hipStream_t s) {
   constexpr int TOK = kThreads / (D / (2 * Vec<T>::N));
   const int64_t tiles = ((int64_t)a.batch * a.seq_len + TOK - 1) / TOK;
   const int heads = a.heads_q + a.heads_kv;
-  const int hb = head_share(tiles, heads);
+  // (a workgroup of 32 tokens reads a run of each head, or, token-major, heads side by side: 32768 tokens of 32 + 8 heads
+  // with 8 and 16 heads a workgroup take 126 and 132 us head-major, 158 and 138 token-major)
+  const int hb = head_share(tiles, heads, a.q.sh < a.q.ss ? 16 : 8);
   const dim3 grid((unsigned)tiles, (unsigned)((heads + hb - 1) / hb));
-  if (a.rope.interleaved) rotate_kernel<T, D, true><<<grid, kThreads, 0, s>>>(a, fast_div(a.seq_len), hb);
-  else rotate_kernel<T, D, false><<<grid, kThreads, 0, s>>>(a, fast_div(a.seq_len), hb);
+  const FastDiv per_b = fast_div(a.seq_len);
+  if (a.rope.interleaved) rotate_kernel<T, D, true, true><<<grid, kThreads, 0, s>>>(a, per_b, hb);
+  else if (a.rope.rot * (int)sizeof(T) % 128 == 0) rotate_kernel<T, D, false, true><<<grid, kThreads, 0, s>>>(a, per_b, hb);
+  else rotate_kernel<T, D, false, false><<<grid, kThreads, 0, s>>>(a, per_b, hb);
   return hipGetLastError();
 }
 
@@ -221,10 +249,12 @@ template <typename T, int D>
 hipError_t append(const AppendArgs& a, hipStream_t s) {
   constexpr int TOK = kThreads / (D / (2 * Vec<T>::N));
   const int64_t tiles = ((int64_t)a.batch * a.tokens + TOK - 1) / TOK;
-  const int hb = head_share(tiles, a.heads_kv);
+  const int hb = head_share(tiles, a.heads_kv, 8);
   const dim3 grid((unsigned)tiles, (unsigned)((a.heads_kv + hb - 1) / hb));
-  if (a.rope.interleaved) append_kernel<T, D, true><<<grid, kThreads, 0, s>>>(a, fast_div(a.tokens), hb);
-  else append_kernel<T, D, false><<<grid, kThreads, 0, s>>>(a, fast_div(a.tokens), hb);
+  const FastDiv per_b = fast_div(a.tokens);
+  if (a.rope.interleaved) append_kernel<T, D, true, true><<<grid, kThreads, 0, s>>>(a, per_b, hb);
+  else if (a.rope.rot * (int)sizeof(T) % 128 == 0) append_kernel<T, D, false, true><<<grid, kThreads, 0, s>>>(a, per_b, hb);
+  else append_kernel<T, D, false, false><<<grid, kThreads, 0, s>>>(a, per_b, hb);
   return hipGetLastError();
 }
 
