@@ -62,7 +62,7 @@ typedef struct {
  * instead, which takes the gradient of the rotated tensors to that of the
  * unrotated ones.  Arithmetic in fp32, rounded once to dtype.
  * SEER_ERR_UNSUPPORTED: head_dim not 64 or 128, a rot_dim that is no multiple of
- * 16, strides that are no multiple of 16 bytes, more than 2^31 - 1 tokens.
+ * 16, strides that are no multiple of 16 bytes, more than 2^27 tokens or 65535 heads.
  */
 seer_status seer_rope(const seer_rope_desc* desc, const seer_rope_params* rope, const void* q, const void* k,
                       void* q_out, void* k_out, const int32_t* positions, int32_t start, int32_t grad,
@@ -86,7 +86,9 @@ typedef struct {
  * A packed batch is batch 1 with a row for each token.  Tokens whose position or row is
  * negative or beyond the table, or whose page is none, are padding: not
  * written.  Every other slot of the cache is left as it is.  Two tokens of a call
- * may not go to the same slot (which of them stays is unspecified then).
+ * may not go to the same slot (which of them stays is unspecified then), and k and v may not lie in
+ * the pools.
+ * SEER_ERR_UNSUPPORTED: as seer_rope, and a table whose rows have room for more than 2^30 tokens.
  */
 seer_status seer_kv_append(const seer_append_desc* desc, const seer_rope_params* rope, const void* k, const void* v,
                            void* k_cache, void* v_cache, const int32_t* table, const int32_t* positions,
@@ -125,7 +127,9 @@ size_t seer_paged_attn_workspace_bytes(const seer_paged_desc* desc);
  * from those of the same sequence in another batch (the cuts lie elsewhere).
  * workspace: device memory of at least seer_paged_attn_workspace_bytes(desc) bytes, 256-byte
  * aligned, not shared with a call that may run at the same time.  Its contents need no set-up.
- * The cache is read once for each 32 query rows (heads_q / heads_kv x tokens).
+ * The cache is read once for each 32 query rows (heads_q / heads_kv x tokens).  o may not overlap an input.
+ * SEER_ERR_UNSUPPORTED: as seer_kv_append, page or slot strides of 64 GB and more, more than 2^23 blocks of 16 query
+ * rows (the sum over batch and heads_kv of heads_q / heads_kv x tokens / 16, each rounded up).
  */
 seer_status seer_paged_attn(const seer_paged_desc* desc, const seer_rope_params* rope, float sm_scale, const void* q,
                             const void* k_cache, const void* v_cache, const int32_t* table,

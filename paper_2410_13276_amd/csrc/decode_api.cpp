@@ -10,7 +10,9 @@
 
 namespace {
 
-constexpr int64_t kMostTokens = (int64_t)1 << 30;  // of one call, and of one table row
+constexpr int64_t kMostTokens = (int64_t)1 << 27;    // of one rope or append call (a launch holds less than 2^32 threads)
+constexpr int64_t kMostKeys = (int64_t)1 << 30;      // of one table row
+constexpr int64_t kMostRows = (int64_t)1 << 23;      // blocks of at least 16 query rows of one KV head, of one attention call
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -55,7 +57,7 @@ seer_status check_rope(const seer_rope_params* r, int32_t head_dim) {
 seer_status check_pages(int32_t page_size, int32_t num_pages, int32_t rows, int32_t max_pages, int64_t table_stride) {
   if (page_size <= 0 || num_pages <= 0 || rows <= 0 || max_pages <= 0) return SEER_ERR_INVALID_ARG;
   if (table_stride < 0) return SEER_ERR_INVALID_ARG;
-  return (int64_t)page_size * max_pages <= kMostTokens ? SEER_OK : SEER_ERR_UNSUPPORTED;
+  return (int64_t)page_size * max_pages <= kMostKeys ? SEER_OK : SEER_ERR_UNSUPPORTED;
 }
 
 seer::TensorView view(const void* p, const int64_t (&st)[3]) { return {p, st[0], st[1], st[2]}; }
@@ -85,9 +87,8 @@ seer_status check_paged(const seer_paged_desc* d) {
   if (s == SEER_OK) s = check_cache_strides(d->v_cache_stride, d->dtype);
   if (s != SEER_OK) return s;
   const int64_t rows = (int64_t)d->heads_q / d->heads_kv * d->tokens;
-  if (rows > kMostTokens || (int64_t)d->batch * d->heads_kv > kMostTokens ||
-      (int64_t)d->batch * d->heads_kv * (rows / 16 + 1) > kMostTokens)
-    return SEER_ERR_UNSUPPORTED;
+  const int64_t blocks = rows / 16 + 1, items = (int64_t)d->batch * d->heads_kv;
+  if (rows > kMostRows || items > kMostRows || items * blocks > kMostRows) return SEER_ERR_UNSUPPORTED;
   return SEER_OK;
 }
 

@@ -64,6 +64,8 @@ def rope_call(B=1, Hq=4, Hkv=2, S=64, D=128, dtype=0, params=rope_params(), q=FA
     (dict(pos_stride=-1), seer.ERR_INVALID_ARG),
     (dict(start=2 ** 31 - 63), seer.ERR_INVALID_ARG),  # the last position would be 2^31
     (dict(B=1 << 16, S=1 << 15), seer.ERR_UNSUPPORTED),
+    (dict(S=(1 << 27) + 1), seer.ERR_UNSUPPORTED),   # a launch holds less than 2^32 threads
+    (dict(Hq=65535), seer.ERR_UNSUPPORTED),
     (dict(params=rope_params(freq=0)), seer.ERR_INVALID_ARG),
     (dict(params=rope_params(freq=FAKE + 4)), seer.ERR_INVALID_ARG),
     (dict(params=rope_params(rot=0)), seer.ERR_INVALID_ARG),
@@ -100,6 +102,8 @@ def append_call(B=2, S=3, H=2, D=128, dtype=0, page=16, pages=8, rows=2, maxp=4,
     (dict(kcs=(0, 2048, 128)), seer.ERR_INVALID_ARG),   # all pages at one place
     (dict(kcs=(4096, 2048, 64)), seer.ERR_INVALID_ARG),  # slots overlap
     (dict(page=1 << 16, maxp=1 << 15), seer.ERR_UNSUPPORTED),  # 2^31 tokens a row
+    (dict(S=(1 << 26) + 1), seer.ERR_UNSUPPORTED),
+    (dict(H=65536), seer.ERR_UNSUPPORTED),
     (dict(params=rope_params(rot=24)), seer.ERR_UNSUPPORTED),
 ])
 def test_append_refuses(kw, status):
@@ -138,7 +142,10 @@ def paged_call(params=None, scale=0.0, q=FAKE, kc=FAKE, vc=FAKE, table=FAKE, pos
     (dict(ts=-1), seer.ERR_INVALID_ARG),
     (dict(ps=-1), seer.ERR_INVALID_ARG),
     (dict(page=1 << 20, maxp=1 << 11), seer.ERR_UNSUPPORTED),
+    (dict(page=1 << 20, maxp=1 << 10, B=0), seer.ERR_INVALID_ARG),
     (dict(B=1 << 20, Hq=4096, Hkv=4096), seer.ERR_UNSUPPORTED),
+    (dict(B=1 << 23), seer.ERR_UNSUPPORTED),         # 2^24 rows of 2 KV heads
+    (dict(cs=(1 << 36, 2048, 128)), seer.ERR_UNSUPPORTED),
     (dict(params=rope_params(rot=8)), seer.ERR_UNSUPPORTED),
 ])
 def test_paged_attention_refuses(kw, status):
