@@ -64,23 +64,33 @@ def _rope_arg(inv_freq, interleaved, scale, dev):
     """seer_rope_params, or None without frequencies."""
     if inv_freq is None:
         return None
-    if inv_freq.dtype is not _t.float64 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+    if inv_freq.dtype is not _t.float64 or inv_freq.stride() != _UNIT:
         raise TypeError("inv_freq must be a contiguous float64 vector (rope_freqs)")
     if inv_freq.get_device() != dev:
         raise ValueError("inv_freq must be on the GPU of the other tensors")
     return _ROPE.pack(inv_freq.data_ptr(), 2 * inv_freq.shape[0], 1 if interleaved else 0, scale)
 
 
-_t = None          # torch, once a call has needed it
+_UNIT, _ZERO = (1,), (0, 0, 0)
+
+# what the first call looks up for all of them
+_t = None           # torch
+_code = None        # torch type -> seer_dtype
+_device = None      # index of the current device
 _raw_stream = None  # device index -> handle of its current stream
+_fn_rope = _fn_append = _fn_paged = _fn_paged_bytes = None
 
 
 def _load():
-    global _t, _raw_stream
-    torch = _seer._torch()
-    # (the handle alone, where this torch offers it: the Stream object around it takes 1 to 3 us)
+    global _t, _code, _device, _raw_stream, _fn_rope, _fn_append, _fn_paged, _fn_paged_bytes
+    torch, lib = _seer._torch(), _seer.lib()
+    _code = {torch.bfloat16: _seer.BF16, torch.float32: _seer.F32}
+    # (where this torch offers it the handle alone: the Stream object around it takes 1 to 3 us)
+    _device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
     _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
         (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
+    _fn_rope, _fn_append = lib.seer_rope, lib.seer_kv_append
+    _fn_paged, _fn_paged_bytes = lib.seer_paged_attn, lib.seer_paged_attn_workspace_bytes
     _t = torch
 
 
@@ -133,9 +143,6 @@ def rope_freqs(rot_dim: int, theta: float = 10000.0, *, scaling: str = "none", f
     return torch.tensor(f, dtype=torch.float64, device=device), scale
 
 
-_ZERO = (0, 0, 0)
-
-
 def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream, grad):
     if _t is None:
         _load()
@@ -165,7 +172,7 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
     if (dev < 0 or qs[-1] != 1 or out is not None
             or k is not None and (k.get_device() != dev or k.dtype is not dtype or ks[-1] != 1)):
         _refuse_tensors(dtype, q=q, k=k, out_q=qo, out_k=ko)
-    if stream is not None or _t.cuda.current_device() != dev:
+    if stream is not None or _device() != dev:
         with _elsewhere(dev, stream):
             return _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, None, grad)
     pos_stride, pos = 0, None
@@ -180,7 +187,9 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
             pos_stride = positions.stride(0)
         pos = positions.data_ptr()
     params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
-    code = _seer._dtype_code(q)
+    code = _code.get(dtype)
+    if code is None:
+        _seer._dtype_code(q)  # raises
     if out is None:
         qo = _t.empty_like(q)
         if k is not None:
@@ -191,8 +200,8 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
     if packed:
         qs, ks, os_, kos = ((0, x[1], x[0]) for x in (qs, ks, os_, kos))
     desc = _ROPE_DESC.pack(batch, heads, kv, seq, dim, code, *qs[:3], *ks[:3], *os_[:3], *kos[:3], pos_stride)
-    status = _seer.lib().seer_rope(desc, params, q.data_ptr(), None if k is None else k.data_ptr(), qo.data_ptr(),
-                                   None if k is None else ko.data_ptr(), pos, start, grad, _raw_stream(dev))
+    status = _fn_rope(desc, params, q.data_ptr(), None if k is None else k.data_ptr(), qo.data_ptr(),
+                      None if k is None else ko.data_ptr(), pos, start, grad, _raw_stream(dev))
     if status:
         _seer._check(status, "seer_rope")
     return qo, ko
@@ -268,7 +277,7 @@ def kv_append(k, v, k_cache, v_cache, table, positions, *, rows=None, inv_freq=N
             or v.dtype is not dtype or k_cache.dtype is not dtype or v_cache.dtype is not dtype
             or k.stride(-1) != 1 or v.stride(-1) != 1 or kcs[-1] != 1 or vcs[-1] != 1):
         _refuse_tensors(dtype, k=k, v=v, k_cache=k_cache, v_cache=v_cache)
-    if stream is not None or _t.cuda.current_device() != dev:
+    if stream is not None or _device() != dev:
         with _elsewhere(dev, stream):
             return kv_append(k, v, k_cache, v_cache, table, positions, rows=rows, inv_freq=inv_freq,
                              interleaved=interleaved, rope_scale=rope_scale)
@@ -277,16 +286,18 @@ def kv_append(k, v, k_cache, v_cache, table, positions, *, rows=None, inv_freq=N
     if rows is not None and _per_token("rows", rows, dev, batch, tokens) != pos_stride and batch > 1:
         raise ValueError("rows must be laid out like positions")
     params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
-    code = _seer._dtype_code(k)
+    code = _code.get(dtype)
+    if code is None:
+        _seer._dtype_code(k)  # raises
     if k.numel() == 0:
         return
     pages, _, page_size, _ = k_cache.shape
     n_rows, max_pages = table.shape
     desc = _CACHE_DESC.pack(batch, tokens, heads, dim, code, page_size, pages, n_rows, max_pages, 0, *ks, *vs,
                             *kcs[:3], *vcs[:3], table.stride(0), pos_stride)
-    status = _seer.lib().seer_kv_append(desc, params, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                        table.data_ptr(), positions.data_ptr(), None if rows is None else rows.data_ptr(),
-                                        _raw_stream(dev))
+    status = _fn_append(desc, params, k.data_ptr(), v.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
+                        table.data_ptr(), positions.data_ptr(), None if rows is None else rows.data_ptr(),
+                        _raw_stream(dev))
     if status:
         _seer._check(status, "seer_kv_append")
 
@@ -306,7 +317,7 @@ def paged_attn_workspace_bytes(q, k_cache, v_cache, table) -> int:
     _, heads, tokens, dim = shape
     desc = _paged_desc(shape, qs, (heads * tokens * dim, tokens * dim, dim), _seer._dtype_code(q), k_cache, v_cache, table,
                        0)
-    return _seer.lib().seer_paged_attn_workspace_bytes(desc)
+    return _fn_paged_bytes(desc)
 
 
 def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interleaved: bool = False,
@@ -325,7 +336,7 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
             or v_cache.dtype is not dtype or q.stride(-1) != 1 or k_cache.stride(-1) != 1 or v_cache.stride(-1) != 1
             or out is not None):
         _refuse_tensors(dtype, q=q, k_cache=k_cache, v_cache=v_cache, out=out)
-    if stream is not None or _t.cuda.current_device() != dev:
+    if stream is not None or _device() != dev:
         with _elsewhere(dev, stream):
             return paged_attn(q, k_cache, v_cache, table, positions, inv_freq=inv_freq, interleaved=interleaved,
                               rope_scale=rope_scale, sm_scale=sm_scale, out=out, lse=lse, want_lse=want_lse,
@@ -337,13 +348,14 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
         raise ValueError("out must be shaped like q")
     pos_stride = _per_token("positions", positions, dev, batch, tokens)
     params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
-    code = _seer._dtype_code(q)
+    code = _code.get(dtype)
+    if code is None:
+        _seer._dtype_code(q)  # raises
     if lse is not None and (lse.shape != q.shape[:-1] or lse.dtype is not _t.float32 or lse.get_device() != dev or
                             not lse.is_contiguous()):
         raise ValueError("lse must be contiguous float32 [batch, heads, tokens] on the GPU of the other tensors")
     if workspace is not None and (workspace.get_device() != dev or not workspace.is_contiguous()):
         raise ValueError("workspace must be contiguous and on the GPU of the other tensors")
-    lib = _seer.lib()
     o = _t.empty_like(q) if out is None else out
     if lse is None and want_lse:
         lse = _t.empty(q.shape[:-1], dtype=_t.float32, device=q.device)
@@ -351,12 +363,11 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
         return o, lse
     desc = _paged_desc(shape, qs, _tokens_of(o, "out")[1], code, k_cache, v_cache, table, pos_stride)
     if workspace is None:
-        need = lib.seer_paged_attn_workspace_bytes(desc)
+        need = _fn_paged_bytes(desc)
         workspace = _t.empty(need or 1, dtype=_t.uint8, device=q.device)
-    status = lib.seer_paged_attn(desc, params, sm_scale, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(),
-                                 table.data_ptr(), positions.data_ptr(), o.data_ptr(),
-                                 None if lse is None else lse.data_ptr(), workspace.data_ptr(),
-                                 workspace.numel() * workspace.element_size(), _raw_stream(dev))
+    status = _fn_paged(desc, params, sm_scale, q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), table.data_ptr(),
+                       positions.data_ptr(), o.data_ptr(), None if lse is None else lse.data_ptr(),
+                       workspace.data_ptr(), workspace.numel() * workspace.element_size(), _raw_stream(dev))
     if status:
         _seer._check(status, "seer_paged_attn")
     return o, lse

@@ -1,0 +1,157 @@
+"""The layouts, page sizes and ways of calling the paged cache that its calls allow, beyond those of the other tests:
+K and V of different layouts or of one buffer, pages as long as a sequence, broadcast operands, rows of their own,
+two streams at once, and two graphs that share a workspace."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+seer = pytest.importorskip("paper_2410_13276_amd")
+
+from decode_ref import assert_rounded, attend, freqs, make_cache, on_gpu, rotate  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
+NAN = float("nan")
+
+
+def _close(o, lse, ref):
+    assert_rounded(o.cpu(), ref[0], ref[2])
+    if lse is not None:
+        got, empty = lse.cpu().double(), ref[1] == -math.inf
+        assert torch.equal(got == -math.inf, empty)
+        assert bool(((got - ref[1]).abs() <= ref[3])[~empty].all())
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+@pytest.mark.parametrize("ps,D", [(12, 64), (100, 128), (2048, 128), (1000, 64), (4, 128)])
+def test_page_sizes_and_mixed_layouts(dtype, ps, D):
+    print(f"[layouts] page {ps} {dtype}", flush=True)
+    gen = torch.Generator().manual_seed(ps)
+    lengths = [1500, 700, 99]
+    kc, vc, table = make_cache(gen, lengths, ps, 2, D, TYPES[dtype], fill=NAN)
+    q = torch.randn(3, 10, 1, D, generator=gen).to(TYPES[dtype])
+    pos = torch.tensor([[n - 1] for n in lengths], dtype=torch.int32)
+    ref = attend(q, kc, vc, table, pos, 0.0)
+    # K head-major, V token-major
+    _close(*seer.paged_attn(q.cuda(), on_gpu(kc), on_gpu(vc, "pshd"), table.cuda(), pos.cuda(), want_lse=True), ref)
+    # K and V halves of one buffer, and a page's heads beside others'
+    both = torch.full((kc.shape[0], 2, 3, ps, D), NAN, dtype=TYPES[dtype])
+    both[:, 0, 1:], both[:, 1, :2] = kc, vc
+    both = both.cuda()
+    _close(*seer.paged_attn(q.cuda(), both[:, 0, 1:], both[:, 1, :2], table.cuda(), pos.cuda(), want_lse=True), ref)
+    # appended to in place, the rest of the buffer left as it is
+    k = torch.randn(3, 2, 1, D, generator=gen).to(TYPES[dtype])
+    before = both.clone()
+    seer.kv_append(k.cuda(), k.cuda(), both[:, 0, 1:], both[:, 1, :2], table.cuda(), pos.cuda())
+    want = before.clone()
+    for b, n in enumerate(lengths):
+        page, slot = int(table[b, (n - 1) // ps]), (n - 1) % ps
+        want[page, 0, 1:, slot], want[page, 1, :2, slot] = k[b, :, 0].cuda(), k[b, :, 0].cuda()
+    assert torch.equal(torch.nan_to_num(both, nan=5.0), torch.nan_to_num(want, nan=5.0))
+
+
+def test_broadcast_operands_and_rows_of_their_own():
+    gen = torch.Generator().manual_seed(3)
+    kc, vc, table = make_cache(gen, [900], 16, 1, 64, torch.bfloat16, fill=NAN)
+    q = torch.randn(1, 1, 1, 64, generator=gen).bfloat16()
+    pos = torch.tensor([[899]], dtype=torch.int32)
+    ref = attend(q, kc, vc, table, pos, 0.0)
+    o, lse = seer.paged_attn(q.cuda().expand(5, 6, 1, 64), kc.cuda(), vc.cuda(), table.cuda().expand(5, -1),
+                             pos.cuda().expand(5, 1), want_lse=True)
+    _close(o, lse, [x.expand(5, 6, *x.shape[2:]) for x in ref])
+    # one position for each sequence of [B, H, 1, D]
+    o1, _ = seer.paged_attn(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), pos[:, 0].cuda())
+    _close(o1, None, ref)
+    # [B, H, S, D] tokens that name their rows: two sequences' tokens in one entry, a broadcast value
+    gk, gv = torch.zeros(6, 2, 8, 64, device="cuda"), torch.zeros(6, 2, 8, 64, device="cuda")
+    tb = torch.tensor([[0, 1], [2, 3], [4, 5]], dtype=torch.int32, device="cuda")
+    k = torch.randn(2, 2, 3, 64, generator=gen)
+    rows = torch.tensor([[2, 0, 2], [1, 1, -1]], dtype=torch.int32, device="cuda")
+    at = torch.tensor([[9, 3, 10], [0, 15, 4]], dtype=torch.int32, device="cuda")
+    seer.kv_append(k.cuda(), torch.ones(1, 1, 1, 64, device="cuda").expand(2, 2, 3, 64), gk, gv, tb, at, rows=rows)
+    want = torch.zeros(6, 2, 8, 64)
+    want[5, :, 1], want[0, :, 3], want[5, :, 2], want[2, :, 0], want[3, :, 7] = \
+        k[0, :, 0], k[0, :, 1], k[0, :, 2], k[1, :, 0], k[1, :, 1]
+    assert torch.equal(gk.cpu(), want) and torch.equal(gv.cpu(), (want != 0).any(-1, keepdim=True).expand_as(want).float())
+    # rope of a broadcast head: every copy turns alike
+    f = freqs(64)
+    x = torch.randn(1, 1, 7, 64, generator=gen)
+    y, _ = seer.rope(x.cuda().expand(2, 4, 7, 64), None, f.cuda(), start=11)
+    ref, err = rotate(x.expand(2, 4, 7, 64), 11 + torch.arange(7)[None, None, :], f)
+    assert_rounded(y.cpu(), ref, err)
+
+
+@pytest.mark.parametrize("dtype", list(TYPES))
+def test_a_row_of_nan_is_alone(dtype):
+    """NaN in one query head spoils its own row, in whole rows and in joined ones, below and above 16 rows."""
+    gen = torch.Generator().manual_seed(9)
+    for heads, n in ((6, 300), (6, 5000), (20, 5000)):
+        kc, vc, table = make_cache(gen, [n, n], 16, 1, 128, TYPES[dtype])
+        q = torch.randn(2, heads, 1, 128, generator=gen).to(TYPES[dtype])
+        pos = torch.full((2, 1), n - 1, dtype=torch.int32)
+        ref = attend(q, kc, vc, table, pos, 0.0)
+        q[0, 3, 0, 5] = NAN
+        o, lse = seer.paged_attn(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), pos.cuda(), want_lse=True)
+        assert bool(torch.isnan(o[0, 3]).all()) and bool(torch.isnan(lse[0, 3]).all())
+        keep = torch.ones(2, heads, dtype=torch.bool)
+        keep[0, 3] = False
+        assert_rounded(o.cpu()[keep], ref[0][keep], ref[2][keep])
+        assert bool(((lse.cpu() - ref[1]).abs() <= ref[3])[keep].all())
+
+
+def test_two_streams_at_once():
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    n, B = 6000, 4
+    kc, vc = (torch.randn(B * 400, 2, 16, 128, device="cuda", generator=gen).bfloat16() for _ in range(2))
+    table = torch.randperm(B * 400, device="cuda", generator=gen).view(B, 400).to(torch.int32)
+    qs = [torch.randn(B, 8, 1, 128, device="cuda", generator=gen).bfloat16() for _ in range(2)]
+    ps = [torch.tensor([[n - 1 - 500 * i - 100 * b] for b in range(B)], dtype=torch.int32, device="cuda") for i in range(2)]
+    want = [seer.paged_attn(q, kc, vc, table, p, want_lse=True) for q, p in zip(qs, ps)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(10):
+        for i, s in enumerate(streams):
+            got[i].append(seer.paged_attn(qs[i], kc, vc, table, ps[i], want_lse=True, stream=s))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for o, lse in got[i]:
+            assert torch.equal(o, want[i][0]) and torch.equal(lse, want[i][1])
+
+
+def test_two_graphs_share_a_workspace():
+    """Replayed one after the other, with eager calls on the same workspace between them."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    kc, vc = (torch.randn(300, 2, 16, 64, device="cuda", generator=gen) for _ in range(2))
+    table = torch.randperm(300, device="cuda", generator=gen).view(1, 300).to(torch.int32)
+    at = torch.tensor([[4000]], dtype=torch.int32, device="cuda")
+    q = [torch.randn(1, h, 1, 64, device="cuda", generator=gen) for h in (4, 16)]
+    out = [torch.empty_like(x) for x in q]
+    ws = torch.empty(max(seer.paged_attn_workspace_bytes(x, kc, vc, table) for x in q), dtype=torch.uint8, device="cuda")
+    step = lambda i, o: seer.paged_attn(q[i], kc, vc, table, at, out=o, workspace=ws)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in range(2):
+            step(i, out[i])
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            step(i, out[i])
+        graphs.append(g)
+    for r in range(4):
+        print(f"[layouts] replay {r}", flush=True)
+        at.fill_(4000 + 150 * r)
+        want = []
+        for i in range(2):
+            want.append(torch.empty_like(q[i]))
+            step(i, want[i])
+        for i in (r % 2, 1 - r % 2):
+            out[i].zero_()
+            graphs[i].replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out[i], want[i])
