@@ -46,9 +46,10 @@ struct Stride16 {
 struct KernelArgs {
   PagedArgs a;
   Stride16 kst, vst;            // strides of the pools, in 16-byte pieces
-  int group, rows, row_blocks;  // G, G tokens, blocks of 16 NT rows
+  int rows, row_blocks;         // G tokens, blocks of 16 NT rows
+  FastDiv group, blocks;        // by G and row_blocks
   int capacity;                 // tokens that a table row has room for
-  int unit;                     // keys per unit
+  int unit_shift;               // log2 of the keys per unit
   bool join;                    // rows may be split: records are written for the second launch
   float scale_log2;
   int2* record;                 // [batch heads_kv row_blocks] first slot and last workgroup of a split row, or -1
@@ -80,27 +81,68 @@ __device__ __forceinline__ int length_of(const KernelArgs& k, int b) {
   return len;
 }
 __device__ __forceinline__ int units_of(const KernelArgs& k, int len) {
-  return max(1, (int)(((uint32_t)len + (uint32_t)k.unit - 1u) / (uint32_t)k.unit));
+  return max(1, (len + (1 << k.unit_shift) - 1) >> k.unit_shift);
 }
 
-// The weights dealt to the workgroups: workgroup w has base (+ 1 for the first `rest`).
+// The weights dealt to the workgroups: workgroup w has base (+ 1 for the first `rest`).  (All below 2^30: the
+// 64-bit divisions that this was first written with were 600 instructions at every workgroup's start.)
 struct Deal {
-  int64_t base, rest;
-  int workers;
-  static __device__ __forceinline__ int64_t quot(int64_t x, int64_t y) {  // (64-bit division takes some 150 instructions)
-    return (x | y) >> 32 ? x / y : (int64_t)((uint32_t)x / (uint32_t)y);
-  }
-  __device__ __forceinline__ Deal(int64_t total, int groups) {
-    workers = (int)min((int64_t)groups, total);
-    base = quot(total, workers);
+  uint32_t base, rest, workers;
+  __device__ __forceinline__ Deal(uint32_t total, uint32_t groups) {
+    workers = min(groups, total);
+    base = total / workers;
     rest = total - base * workers;
   }
-  __device__ __forceinline__ int64_t first(int w) const { return w * base + min((int64_t)w, rest); }
-  __device__ __forceinline__ int owner(int64_t x) const {
-    const int64_t big = rest * (base + 1);
-    return (int)(x < big ? quot(x, base + 1) : rest + quot(x - big, base));
+  __device__ __forceinline__ int first(uint32_t w) const { return (int)(w * base + min(w, rest)); }
+  __device__ __forceinline__ int owner(uint32_t x) const {
+    const uint32_t big = rest * (base + 1);
+    return (int)(x < big ? x / (base + 1) : rest + (x - big) / base);
   }
 };
+
+// Within a wavefront, without the LDS: inclusive prefix sum; least of a row of 16 lanes; largest and sum of the
+// lanes l % 16.
+template <int CTRL, int ROWS = 0xf>
+__device__ __forceinline__ int dpp(int old, int x) {
+  return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_prefix(int x) {
+  x += dpp<0x111>(0, x);  // row_shr 1, 2, 4, 8
+  x += dpp<0x112>(0, x);
+  x += dpp<0x114>(0, x);
+  x += dpp<0x118>(0, x);
+  x += dpp<0x142, 0xa>(0, x);  // row_bcast 15 to rows 1 and 3
+  x += dpp<0x143, 0xc>(0, x);  // row_bcast 31 to rows 2 and 3
+  return x;
+}
+__device__ __forceinline__ int row_min(int x) {
+  x = min(x, dpp<0xb1>(x, x));   // quad_perm 1 0 3 2
+  x = min(x, dpp<0x4e>(x, x));   // quad_perm 2 3 0 1
+  x = min(x, dpp<0x141>(x, x));  // row_half_mirror
+  return min(x, dpp<0x140>(x, x));  // row_mirror
+}
+typedef __attribute__((ext_vector_type(2))) unsigned int u32pair;
+__device__ __forceinline__ void across(float x, bool half, float& y, float& z) {
+  const uint32_t u = __float_as_uint(x);
+  const u32pair p = half ? __builtin_bit_cast(u32pair, __builtin_amdgcn_permlane32_swap(u, u, false, false))
+                         : __builtin_bit_cast(u32pair, __builtin_amdgcn_permlane16_swap(u, u, false, false));
+  y = __uint_as_float(p[0]);
+  z = __uint_as_float(p[1]);
+}
+__device__ __forceinline__ float column_max(float x) {
+  float y, z;
+  across(x, false, y, z);
+  x = fmaxf(y, z);
+  across(x, true, y, z);
+  return fmaxf(y, z);
+}
+__device__ __forceinline__ float column_sum(float x) {
+  float y, z;
+  across(x, false, y, z);
+  x = y + z;
+  across(x, true, y, z);
+  return y + z;
+}
 
 __device__ __forceinline__ void unpack8(const u32x4 (&q)[1], float (&y)[8]) {
 #pragma unroll
@@ -114,26 +156,23 @@ __device__ __forceinline__ void unpack8(const u32x4 (&q)[2], float (&y)[8]) {
   for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(q[i / 4][i % 4]);
 }
 
-// Elements d0 .. d0 + 7 of a head, y, rotated at position pos; z: the other half of their planes (half layout).
-__device__ __forceinline__ void rotate8(const RopeView& r, const TurnRate* rate, int d0, int pos, float (&y)[8],
-                                        const float (&z)[8]) {
-  const bool second = d0 >= r.rot / 2;
+// Elements d0 .. d0 + 7 of a head, y, rotated; z: the other half of their planes (half layout), cs: cosine and sine of the
+// token's planes.
+__device__ __forceinline__ void rotate8(const RopeView& r, const float2* cs, int d0, float (&y)[8], const float (&z)[8]) {
+  if (r.interleaved) {
 #pragma unroll
-  for (int i = 0; i < 8; i += 2) {
-    float co[2], si[2];
-    if (r.interleaved) {
-      turn_cos_sin(rate[(d0 + i) / 2], pos, co[0], si[0]);
-      co[0] *= r.scale;
-      si[0] *= r.scale;
-      const float u = y[i], v = y[i + 1];
-      y[i] = u * co[0] - v * si[0];
-      y[i + 1] = u * si[0] + v * co[0];
-    } else {
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = cs[d0 / 2 + i];
+      const float u = y[2 * i], v = y[2 * i + 1];
+      y[2 * i] = u * f.x - v * f.y;
+      y[2 * i + 1] = u * f.y + v * f.x;
+    }
+  } else {
+    const bool second = d0 >= r.rot / 2;
 #pragma unroll
-      for (int f = 0; f < 2; ++f) {
-        turn_cos_sin(rate[(second ? d0 - r.rot / 2 : d0) + i + f], pos, co[f], si[f]);
-        y[i + f] = y[i + f] * (co[f] * r.scale) + z[i + f] * ((second ? si[f] : -si[f]) * r.scale);
-      }
+    for (int i = 0; i < 8; ++i) {
+      const float2 f = cs[(second ? d0 - r.rot / 2 : d0) + i];
+      y[i] = y[i] * f.x + z[i] * (second ? f.y : -f.y);
     }
   }
 }
@@ -158,23 +197,30 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   constexpr int kRowCost = NT;
   constexpr int OSTR = D + 4;
   constexpr int QJ = BF ? D / 32 : D / 16;
-  // the operand Q^T as the lanes read it, then the wavefronts' results
+  // the operand Q^T as the lanes read it and the tokens' cosines and sines, then the wavefronts' results
   __shared__ union {
-    u32x4 q[QP][NT][QJ][kWave];
+    struct {
+      u32x4 q[QP][NT][QJ][kWave];
+      float2 cs[ROWS][D / 2];
+    };
     float o[kWaves][ROWS][OSTR];
   } sh;
   __shared__ float sM[kWaves][ROWS], sL[kWaves][ROWS];
-  __shared__ TurnRate sRate[64];
 
   const PagedArgs& a = ka.a;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
   const int n = lane % 16, g = lane / 16;
   const int items = a.heads_kv * ka.row_blocks;  // rows of a sequence
+  const int group = ka.group.d;
   const float c = ka.scale_log2;
 
-  const bool rope = a.rope.freq != nullptr;
-  if (rope && tid < a.rope.rot / 2) sRate[tid] = turn_rate(a.rope.freq[tid]);
+  // (every line of the arguments is fetched now, not when it is first needed)
+  asm volatile("" ::"s"(a.osb), "s"(a.kc.ptr), "s"(a.table.ptr), "s"(a.batch), "s"(ka.kst.page), "s"(ka.part_o));
+
+  const bool rope = QP == 2 || (!BF && a.rope.freq != nullptr);
+  // angle per position of plane `lane` (no branch around the load: it would be waited for at once)
+  const double freq = (rope ? a.rope.freq : (const double*)a.kc.ptr)[rope ? min(lane, a.rope.rot / 2 - 1) : 0];
 
   // ---- this workgroup's share.  Every wavefront works it out by itself: a lane sums the weights of some
   // sequences in a row, and a scan over the lanes finds the sequence that the share begins in.
@@ -185,31 +231,28 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
     my_len = length_of(ka, i);
     mine += units_of(ka, my_len) + kRowCost;
   }
-  int upto = mine;  // inclusive prefix over the lanes
-#pragma unroll
-  for (int off = 1; off < kWave; off <<= 1) {
-    const int y = __shfl_up(upto, off);
-    if (lane >= off) upto += y;
-  }
+  const int upto = wave_prefix(mine);
+  TurnRate rate = turn_rate(freq);
+  asm volatile("" : "+v"(rate.hi), "+v"(rate.lo));  // (here: the positions' wait was its wait too; later it would be the tile's)
   const int w = blockIdx.x;
-  const Deal deal((int64_t)__builtin_amdgcn_readlane(upto, kWave - 1) * items, (int)gridDim.x);
-  if (w >= deal.workers) return;
-  int64_t x = deal.first(w);
-  const int64_t x_end = deal.first(w + 1);
-  const int owner_lane = (int)__popcll(__ballot((int64_t)upto * items <= x));
+  const Deal deal((uint32_t)(__builtin_amdgcn_readlane(upto, kWave - 1) * items), gridDim.x);
+  if (w >= (int)deal.workers) return;
+  int x = deal.first(w);
+  const int x_end = deal.first(w + 1);
+  const int owner_lane = (int)__popcll(__ballot(upto * items <= x));
   int b = owner_lane * share;
-  int64_t off = x - (int64_t)(__builtin_amdgcn_readlane(upto, owner_lane) - __builtin_amdgcn_readlane(mine, owner_lane)) * items;
+  int off = x - (__builtin_amdgcn_readlane(upto, owner_lane) - __builtin_amdgcn_readlane(mine, owner_lane)) * items;
   int len = share == 1 ? __builtin_amdgcn_readlane(my_len, owner_lane) : length_of(ka, b);
   int row_units = units_of(ka, len);
-  while (off >= (int64_t)(row_units + kRowCost) * items) {
-    off -= (int64_t)(row_units + kRowCost) * items;
+  while (off >= (row_units + kRowCost) * items) {
+    off -= (row_units + kRowCost) * items;
     len = length_of(ka, ++b);
     row_units = units_of(ka, len);
   }
   len = __builtin_amdgcn_readfirstlane(len);
   row_units = __builtin_amdgcn_readfirstlane(row_units);
-  int item = (int)off / (row_units + kRowCost);      // (off is below 2^30)
-  int at_w = (int)off - item * (row_units + kRowCost);  // position within the row's weight
+  int item = (int)((uint32_t)off / (uint32_t)(row_units + kRowCost));
+  int at_w = off - item * (row_units + kRowCost);  // position within the row's weight
 
   // ---- a run of one row's units [u0, u1): where it is, and its first tile
   int u0, u1, h, key0, k_hi;
@@ -305,35 +348,40 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   constexpr int QN = (ROWS * (D / 8) + kThreads - 1) / kThreads;
   constexpr int QW = BF ? 1 : 2;  // 16-byte pieces of 8 elements
   u32x4 q_own[QN][QW], q_other[QN][QW];
-  int q_pos[QN];
+  int col_pos[NT], rope_pos;  // positions of the columns' tokens, and of the block's token that this wavefront turns first
   // The next run of the share, with its first tile on the way; false when the share is done.
   auto begin = [&]() -> bool {
     for (;;) {
       if (x >= x_end) return false;
-      const int take = (int)min((int64_t)(row_units + kRowCost - at_w), x_end - x);
+      const int take = min(row_units + kRowCost - at_w, x_end - x);
       u0 = max(at_w - kRowCost, 0);
       u1 = max(at_w + take - kRowCost, 0);
       if (u1 > u0) break;
       x += take;  // (a row's cost alone)
       at_w += take;
     }
-    h = item / ka.row_blocks;
-    key0 = (int)min((int64_t)u0 * ka.unit, (int64_t)len) + wave * S::KT;
-    k_hi = (int)min((int64_t)u1 * ka.unit, (int64_t)len);
+    h = fast_quot(ka.blocks, item);
+    key0 = (u0 << ka.unit_shift) + wave * S::KT;
+    k_hi = u1 == row_units ? len : u1 << ka.unit_shift;
     // a lane's piece of a K row: 16 bytes at 16 g of each 64; of a V row: 16 (8: bf16 of head_dim 64) at its share n
     kbase = (const char*)((const T*)a.kc.ptr + h * a.kc.sh) + 16 * g;
     vbase = (const char*)((const T*)a.vc.ptr + h * a.vc.sh) + (BF ? 4 * S::VW : 16) * n;
     table = a.table.ptr + b * a.table.stride;
     const Pages pg = pages(key0);
     pn = pages(key0 + STEP);
+    // (all that the run needs before its first scores is asked for ahead of the tile, which it would wait for otherwise)
+    const int32_t* pos_b = a.positions + b * a.pos_stride;
+    const int r0 = (item - h * ka.row_blocks) * ROWS;
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) col_pos[ct] = pos_b[fast_quot(ka.group, min(r0 + 16 * ct + n, ka.rows - 1))];
+    rope_pos = pos_b[min(fast_quot(ka.group, r0) + wave, a.tokens - 1)];
 #pragma unroll
     for (int i = 0; i < QN; ++i) {
       const int e = tid + i * kThreads, rl = e / (D / 8), d0 = e % (D / 8) * 8;
-      const int r = min((item - h * ka.row_blocks) * ROWS + rl, ka.rows - 1), tk = r / ka.group;
-      const T* src = (const T*)a.q.ptr + b * a.q.sb + (h * ka.group + (r - tk * ka.group)) * a.q.sh + tk * a.q.ss;
+      const int r = min(r0 + rl, ka.rows - 1), tk = fast_quot(ka.group, r);
+      const T* src = (const T*)a.q.ptr + b * a.q.sb + (h * group + (r - tk * group)) * a.q.sh + tk * a.q.ss;
       const int half = a.rope.rot / 2;
       const bool turns = rope && d0 < a.rope.rot;
-      if (turns) q_pos[i] = a.positions[b * a.pos_stride + tk];
       const T* other = src + (turns && !a.rope.interleaved ? (d0 < half ? d0 + half : d0 - half) : d0);
 #pragma unroll
       for (int f = 0; f < QW; ++f) {
@@ -347,25 +395,37 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   };
   bool busy = begin();
   bool first_run = true;
-  if (rope) __syncthreads();  // sRate is set
 
   while (busy) {
     const int r0 = (item - h * ka.row_blocks) * ROWS;  // the first row of the block
     const int32_t* pos_b = a.positions + b * a.pos_stride;
 
-    // ---- Q^T to LDS
+    // ---- Q^T to LDS, rotated: a lane forms its plane's cosine and sine of a token, for all heads
+    const int t_first = fast_quot(ka.group, r0);  // of the block's tokens
+    if (rope) {
+      const int t_last = fast_quot(ka.group, min(r0 + ROWS, ka.rows) - 1);
+      if (lane < a.rope.rot / 2) {
+        for (int tk = t_first + wave; tk <= t_last; tk += kWaves) {
+          float co, si;
+          turn_cos_sin(rate, tk == t_first + wave ? rope_pos : pos_b[tk], co, si);
+          sh.cs[tk - t_first][lane] = make_float2(co * a.rope.scale, si * a.rope.scale);
+        }
+      }
+      __syncthreads();
+    }
 #pragma unroll
     for (int i = 0; i < QN; ++i) {
       const int e = tid + i * kThreads, rl = e / (D / 8), d0 = e % (D / 8) * 8;
       if (rl >= ROWS) break;
       const bool turns = rope && d0 < a.rope.rot;
+      const float2* cs = sh.cs[fast_quot(ka.group, min(r0 + rl, ka.rows - 1)) - t_first];
       if constexpr (BF) {
         const int j = d0 / 32, at = d0 % 32 / 8 * 16 + rl % 16;
         if constexpr (QP == 2) {
           float y[8], z[8];
           unpack8(q_own[i], y);
           unpack8(q_other[i], z);
-          if (turns) rotate8(a.rope, sRate, d0, q_pos[i], y, z);
+          if (turns) rotate8(a.rope, cs, d0, y, z);
           bf16x8 hi, lo;
 #pragma unroll
           for (int f = 0; f < 8; ++f) {
@@ -382,7 +442,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
         float y[8], z[8];
         unpack8(q_own[i], y);
         unpack8(q_other[i], z);
-        if (turns) rotate8(a.rope, sRate, d0, q_pos[i], y, z);
+        if (turns) rotate8(a.rope, cs, d0, y, z);
 #pragma unroll
         for (int f = 0; f < 2; ++f)
           sh.q[0][rl / 16][j][at + 16 * f] = u32x4{__float_as_uint(y[4 * f]), __float_as_uint(y[4 * f + 1]),
@@ -390,21 +450,21 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
       }
     }
 
-    // ---- the columns: rows r0 + 16 ct + n, the last key each sees
+    // ---- the columns: rows r0 + 16 ct + n, the last key each sees.  Keys below `even` are seen alike by all live rows
+    // (where no row is live, none matters): with one token a sequence, all of them.
     int last[NT], token[NT];
-    int least = 0x7fffffff;
+    int even = k_hi;
+    if (a.tokens > 1) {
+      int least = 0x7fffffff;
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct) {
-      const int r = min(r0 + 16 * ct + n, ka.rows - 1);
-      token[ct] = r / ka.group;
-      last[ct] = min(pos_b[token[ct]], ka.capacity - 1);
-      if (last[ct] >= 0) least = min(least, last[ct]);
+      for (int ct = 0; ct < NT; ++ct) {
+        token[ct] = fast_quot(ka.group, min(r0 + 16 * ct + n, ka.rows - 1));
+        last[ct] = min(col_pos[ct], ka.capacity - 1);
+        if (last[ct] >= 0) least = min(least, last[ct]);
+      }
+      least = __builtin_amdgcn_readfirstlane(row_min(least));
+      if (least < len - 1) even = min(k_hi, (least + 1) / S::KT * S::KT);
     }
-#pragma unroll
-    for (int off = 1; off < 16; off <<= 1) least = min(least, __shfl_xor(least, off));
-    // keys below `even` are seen alike by all live rows (where no row is live, none matters)
-    const int common = __builtin_amdgcn_readfirstlane(least) < len ? __builtin_amdgcn_readfirstlane(least) + 1 : len;
-    const int even = common == len ? k_hi : min(k_hi, common / S::KT * S::KT);
     __syncthreads();
 
     f32x4 acc[NT][NA];
@@ -450,8 +510,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
       float mx = s[0];
 #pragma unroll
       for (int e = 1; e < S::PK; ++e) mx = fmaxf(mx, s[e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      mx = column_max(mx);
       if (__ballot(mx > m[ct]) != 0) {
         const float m_new = fmaxf(m[ct], mx);
         const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[ct] - m_new) * c);
@@ -561,8 +620,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
         for (int e = 0; e < S::PK; ++e) s[e] = (t.there >> e & 1) && lane_key + e <= last[ct] ? s[e] : -INFINITY;
         softmax(ct, s);
         const Weights w = weights(s);
-        const int t_lo = min(r0 + 16 * ct, ka.rows - 1) / ka.group;
-        const int t_hi = min(r0 + 16 * ct + 15, ka.rows - 1) / ka.group;
+        const int t_lo = fast_quot(ka.group, min(r0 + 16 * ct, ka.rows - 1));
+        const int t_hi = fast_quot(ka.group, min(r0 + 16 * ct + 15, ka.rows - 1));
         for (int tk = t_lo; tk <= t_hi; ++tk) {
           const int end = max(min(pos_b[tk], ka.capacity - 1), -1) + 1;  // the token's keys
           const uint32_t seen = t.there & ((1u << min(max(end - lane_key, 0), S::PK)) - 1u);
@@ -585,8 +644,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
 
     // ---- the next run, its first tile in flight under this one's end
     const int cur_b = b, cur_item = item, cur_h = h;
+    bool dead[NT];  // (a token at a negative position: no weight, whatever its columns held)
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) dead[ct] = col_pos[ct] < 0;
     const bool opens = u0 == 0, whole = opens && u1 == row_units;
-    const int64_t row_last = x - at_w + row_units + kRowCost - 1;  // the row's last unit
+    const int row_last = x - at_w + row_units + kRowCost - 1;  // the row's last unit
     const int done = u1 + kRowCost - at_w;
     x += done;
     at_w += done;
@@ -608,12 +670,11 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
     __syncthreads();  // sh.q is read
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) {
-      l[ct] += __shfl_xor(l[ct], 16);
-      l[ct] += __shfl_xor(l[ct], 32);
+      l[ct] = column_sum(l[ct]);
       const int col = 16 * ct + n;
       if (g == 0) {
-        sM[wave][col] = m[ct];
-        sL[wave][col] = l[ct];
+        sM[wave][col] = dead[ct] ? -INFINITY : m[ct];
+        sL[wave][col] = dead[ct] ? 0.f : l[ct];
       }
       if (col < nrows)
 #pragma unroll
@@ -644,8 +705,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
         if (d == 0) ka.part_ml[(int64_t)slot * ROWS + rl] = make_float2(mx, sum);
         continue;
       }
-      const int r = r0 + rl, tk = r / ka.group, hq = cur_h * ka.group + (r - tk * ka.group);
-      const bool none = sum == 0.f || pos_b[tk] < 0;
+      const int r = r0 + rl, tk = fast_quot(ka.group, r), hq = cur_h * group + (r - tk * group);
+      const bool none = sum == 0.f;
       const float inv = none ? 0.f : 1.f / sum;
       T* out = (T*)a.o + cur_b * a.osb + hq * a.osh + tk * a.oss + d;
 #pragma unroll
@@ -678,12 +739,12 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka,
   __shared__ float2 sT[JR];
   __shared__ __attribute__((aligned(16))) float sO[GRP][JR][D];
   const PagedArgs& a = ka.a;
-  const int64_t at = blockIdx.x;
-  const int2 rec = ka.record[at];
+  asm volatile("" ::"s"(a.osb), "s"(a.lse), "s"(a.batch), "s"(ka.rows), "s"(ka.part_o));  // (as in the kernel before)
+  const int2 rec = ka.record[blockIdx.x];
   if (rec.x < 0) return;
   const int items = a.heads_kv * ka.row_blocks;
-  const int b = (int)(at / items), item = (int)(at - (int64_t)b * items);
-  const int h = item / ka.row_blocks, rb = item - h * ka.row_blocks;
+  const int b = blockIdx.x / (uint32_t)items, item = blockIdx.x - b * items;
+  const int h = fast_quot(ka.blocks, item), rb = item - h * ka.row_blocks;
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int nrows = min(rows_block, ka.rows - rb * rows_block);
   const int w0 = rec.x / 2, parts = rec.y - w0 + 1;
@@ -734,8 +795,8 @@ __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka,
   for (int i = 1; i < GRP; ++i) o += *(const f32x4*)&sO[i][jr][d];
   mx = sT[jr].x;
   sum = sT[jr].y;
-  const int r = rb * rows_block + rl, t = r / ka.group, hq = h * ka.group + (r - t * ka.group);
-  const bool none = sum == 0.f || a.positions[b * a.pos_stride + t] < 0;
+  const int r = rb * rows_block + rl, t = fast_quot(ka.group, r), hq = h * ka.group.d + (r - t * ka.group.d);
+  const bool none = sum == 0.f;
   T* out = (T*)a.o + b * a.osb + hq * a.osh + t * a.oss + d;
 #pragma unroll
   for (int f = 0; f < 4; ++f) {
@@ -804,19 +865,19 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   const int piece = a.bf16 ? 8 : 4;
   k.kst = {(uint32_t)(a.kc.sp / piece), (uint32_t)(a.kc.ss / piece)};
   k.vst = {(uint32_t)(a.vc.sp / piece), (uint32_t)(a.vc.ss / piece)};
-  k.group = p.group;
+  k.group = fast_div(p.group);
+  k.blocks = fast_div(p.row_blocks);
   k.rows = p.rows;
   k.row_blocks = p.row_blocks;
   k.capacity = a.table.max_pages * a.table.page.d;  // (at most 2^30: no sum of keys overflows)
-  const int step = kWaves * (a.bf16 ? 32 : 16);
   const int64_t items = (int64_t)a.heads_kv * p.row_blocks;
-  int64_t unit = step;
   k.join = k.capacity > kWholeKeys;
-  if (!k.join) unit = (k.capacity + step - 1) / step * step;
-  // (weights stay below 2^31)
-  auto units = [&]() { return (k.capacity + unit - 1) / unit; };
-  while ((units() + 2) * std::max((int64_t)a.batch, items) > INT32_MAX / 2 && unit < (1 << 29)) unit *= 2;
-  k.unit = (int)unit;
+  // a unit is a tile for each wavefront; a whole row where rows are not split, and more where the weights of all units
+  // would not stay below 2^30
+  k.unit_shift = a.bf16 ? 7 : 6;
+  static_assert(kWaves == 4, "128 keys of bf16, 64 of fp32");
+  auto units = [&]() -> int64_t { return ((int64_t)k.capacity + ((int64_t)1 << k.unit_shift) - 1) >> k.unit_shift; };
+  while ((!k.join && units() > 1) || (units() + 2) * items * a.batch > (1 << 30)) ++k.unit_shift;
   k.scale_log2 = a.scale * kLog2e;
   char* ws = (char*)a.workspace;
   k.record = (int2*)ws;
