@@ -4,27 +4,32 @@
 // G = heads_q / heads_kv heads (times the tokens, where a few drafted ones come
 // together) are the columns of one matrix product with the cache: S^T = K Q^T,
 // O^T = V^T P^T.  That is at most 2 * 32 operations a cached element, far below
-// what the matrix cores do in the time HBM takes to bring it: the kernel is bound by
-// reading K and V once, and everything else is arranged around that.
+// what the matrix cores do in the time HBM takes to bring it (they are busy 7% of the time with 4
+// columns): the kernel is bound by reading K and V once, and everything else is arranged around
+// that.  A token after 131072 tokens (32 / 8 heads of 128, bf16) reads 537 MB in 93 us, 64 sequences of 200 to 16000
+// tokens 955 MB in 168 us (5.8 and 5.7 TB/s; a kernel that only reads takes 87 and 159 us, a copy moves 5.1 TB/s).
+// Without any of the arithmetic the first takes 1% less.
 //
-// Work.  The keys of every (sequence, KV head) are cut into units; all units of the
-// call, in (sequence, head, key) order, are dealt out evenly to the workgroups, each
-// taking one contiguous run.  Lengths are read on the device: unequal sequences
+// Work.  The keys of every (sequence, KV head) are cut into units of a tile for each
+// wavefront; all units of the call, in (sequence, head, key) order, are dealt out evenly to the
+// workgroups, each taking one contiguous run.  Lengths are read on the device: unequal sequences
 // balance themselves, and a captured launch stays right as they grow.  A run
 // covers whole rows (their results are written at once) and at most one row's end
 // and one row's beginning, which go to the workspace as partial results (O, running
-// maximum, sum) and are joined in a fixed order by a second launch.
+// maximum, sum) and are joined in a fixed order by a second launch (no counter to set up, and the
+// same bits every time).
 //
 // A wavefront takes KT keys at a time (32 in bf16, 16 in fp32), its lanes holding K
 // rows as the operand of S^T with no LDS in between: lane l reads 16-byte
 // pieces of key row l % 16.  V arrives row-wise, 16 lanes to a row, and is the operand of
 // O^T after an 8 x 8 transposition of 16-bit values in registers (bf16; fp32 operands hold one
 // value, and need none).  The keys' order within a tile is chosen so that a lane's
-// scores S^T are the very ones that its operand P^T of the second product needs.
+// scores S^T are the very ones that its operand P^T of the second product needs.  Only Q^T is read
+// from the LDS, a tile at a time: the registers hold the tile, the accumulators and loads in flight.
 //
 // Precision: fp32 statistics and sums.  In bf16, P enters the second product in two
 // bf16 parts, and so does a q that is rotated here: the matrix cores are idle most of
-// the time, and o is then rounded once.
+// the time (the second part of P costs nothing at 4 columns, 4 us of 56 at 28), and o is then rounded once.
 #include <algorithm>
 
 #include "decode.h"
@@ -36,7 +41,11 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kWorkers = 512;   // workgroups at most: two for each CU
-constexpr int kWholeKeys = 512; // caches of at most this many tokens a sequence are never split
+// Rows are not split, and the second launch not made, where a row has room for so many keys at most (fp32: half), and
+// for twice as many where 128 rows or more, but not more than workgroups, share the launch.  Whole against split, 32 / 8
+// heads of 128: 1 sequence of 400 tokens 9.7 and 11.2 us, of 900 14.2 and 11.4; 16 of 900 16.0 and 18.9; 64 of 900 47.3 and
+// 48.6; fp32, 8 / 8 heads of 64, 1 of 400 10.9 and 9.3, 64 of 400 20.5 and 22.5.
+constexpr int kWholeKeys = 512;
 constexpr float kLn2 = 0.6931471805599453f;
 
 struct Stride16 {
@@ -730,7 +739,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
 // Rows whose keys several workgroups shared: their partial results, in the order of the keys.  A workgroup joins JR
 // rows of an item, a wavefront forming the weights of a row (or part of one: all four then form the same); a thread sums
 // 4 features over the parts grp, grp + GRP, ..  Four rows a workgroup keep a large batch's launch short, one row leaves
-// fewer parts to each thread where the call has few rows (a token after 131072 tokens, 32 heads of 64 parts: 7.3 -> 3.9 us).
+// fewer parts to each thread where the call has few rows (a token after 131072 tokens, 32 rows of 64 parts: 6.9 -> 4.8 us).
 constexpr int kJoinThreads = 256;
 template <typename T, int D, int JR>
 __global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka, int rows_block) {
@@ -871,19 +880,20 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s) {
   k.row_blocks = p.row_blocks;
   k.capacity = a.table.max_pages * a.table.page.d;  // (at most 2^30: no sum of keys overflows)
   const int64_t items = (int64_t)a.heads_kv * p.row_blocks;
-  k.join = k.capacity > kWholeKeys;
+  const int64_t rows = items * a.batch;  // a KV head's, as the workgroups take them
+  k.join = k.capacity > (a.bf16 ? kWholeKeys : kWholeKeys / 2) * (rows >= 128 && rows <= kWorkers ? 2 : 1);
   // a unit is a tile for each wavefront; a whole row where rows are not split, and more where the weights of all units
   // would not stay below 2^30
   k.unit_shift = a.bf16 ? 7 : 6;
   static_assert(kWaves == 4, "128 keys of bf16, 64 of fp32");
   auto units = [&]() -> int64_t { return ((int64_t)k.capacity + ((int64_t)1 << k.unit_shift) - 1) >> k.unit_shift; };
-  while ((!k.join && units() > 1) || (units() + 2) * items * a.batch > (1 << 30)) ++k.unit_shift;
+  while ((!k.join && units() > 1) || (units() + 2) * rows > (1 << 30)) ++k.unit_shift;
   k.scale_log2 = a.scale * kLog2e;
   char* ws = (char*)a.workspace;
   k.record = (int2*)ws;
   k.part_ml = (float2*)(ws + p.ml);
   k.part_o = (float*)(ws + p.o);
-  const dim3 grid((unsigned)std::min((int64_t)kWorkers, units() * items * a.batch));
+  const dim3 grid((unsigned)std::min((int64_t)kWorkers, units() * rows));
   if (a.bf16) return a.head_dim == 128 ? launch_typed<uint16_t, 128>(k, p.nt, grid, s) : launch_typed<uint16_t, 64>(k, p.nt, grid, s);
   return a.head_dim == 128 ? launch_typed<float, 128>(k, p.nt, grid, s) : launch_typed<float, 64>(k, p.nt, grid, s);
 }
