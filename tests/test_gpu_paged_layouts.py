@@ -160,12 +160,12 @@ def test_two_graphs_share_a_workspace():
 @pytest.mark.parametrize("dtype", list(TYPES))
 @pytest.mark.parametrize("batch,most", [(64, 1008), (64, 1040), (256, 1024), (257, 500), (3, 512), (3, 256), (3, 272)])
 def test_both_sides_of_the_rows_that_are_not_split(dtype, batch, most):
-    """Table rows with room for `most` keys, two KV heads: launches that keep every row whole and launches that split them,
+    """Table rows of the pages that `most` keys need, two KV heads: launches that keep every row whole and launches that split them,
     by the room, the number of rows and the type."""
     gen = torch.Generator().manual_seed(batch + most)
     lengths = [int(x) for x in torch.randint(0, 60, (batch,), generator=gen)]
     lengths[0], lengths[-1], lengths[batch // 2] = most, most - 7, most // 2
-    kc, vc, table = make_cache(gen, lengths, 16, 2, 64, TYPES[dtype], wide=most // 16, fill=NAN)
+    kc, vc, table = make_cache(gen, lengths, 16, 2, 64, TYPES[dtype], wide=-(-most // 16), fill=NAN)
     q = torch.randn(batch, 4, 1, 64, generator=gen).to(TYPES[dtype])
     pos = (torch.tensor(lengths) - 1).to(torch.int32)[:, None]
     _close(*seer.paged_attn(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), pos.cuda(), want_lse=True),
