@@ -21,8 +21,8 @@
  * angle t inv_freq[p]; its two elements are (p, p + rot_dim / 2), or (2p, 2p + 1)
  * when interleaved.  Elements from rot_dim on are left as they are:
  *   x' = scale (x cos a - y sin a),  y' = scale (x sin a + y cos a)
- * Angles are reduced to a turn exactly (64-bit fixed point) before the sine, so
- * positions up to 2^31 - 1 keep full fp32 accuracy.
+ * Angles are reduced to a turn in 64-bit fixed point before the sine: off by 2^-52 of
+ * the angle at most, less than fp32's rounding up to 2^27 radians and 5e-7 at 2^31.
  *
  * Paged cache.  A pool of num_pages pages of page_size slots for each of K and V,
  * [page][head][slot][head_dim] with element strides given per (page, head,
@@ -71,7 +71,7 @@ seer_status seer_rope(const seer_rope_desc* desc, const seer_rope_params* rope, 
 typedef struct {
   int32_t batch, tokens, heads_kv, head_dim, dtype;
   int32_t page_size, num_pages;      /* both >= 1 */
-  int32_t table_rows, max_pages;     /* table: device [table_rows][max_pages] */
+  int32_t table_rows, max_pages;     /* table: device [table_rows][max_pages], both >= 1 */
   int32_t reserved;                  /* 0 */
   int64_t k_stride[3], v_stride[3];  /* new tokens: (batch, head, token) */
   int64_t k_cache_stride[3], v_cache_stride[3]; /* (page, head, slot) */
@@ -97,7 +97,7 @@ seer_status seer_kv_append(const seer_append_desc* desc, const seer_rope_params*
 typedef struct {
   int32_t batch, heads_q, heads_kv, tokens, head_dim, dtype; /* heads_q % heads_kv == 0 */
   int32_t page_size, num_pages;      /* both >= 1 */
-  int32_t max_pages;                 /* table: device [batch][max_pages] */
+  int32_t max_pages;                 /* table: device [batch][max_pages], >= 1 */
   int32_t reserved;                  /* 0 */
   int64_t q_stride[3], o_stride[3];  /* (batch, head, token) */
   int64_t k_cache_stride[3], v_cache_stride[3]; /* (page, head, slot) */

@@ -143,6 +143,18 @@ def rope_freqs(rot_dim: int, theta: float = 10000.0, *, scaling: str = "none", f
     return torch.tensor(f, dtype=torch.float64, device=device), scale
 
 
+def _positions_of(t, batch, seq, packed):
+    """Batch stride of rope()'s positions."""
+    n, st = t.shape, t.stride()
+    if n[-1:] == (seq,) and (st[-1] == 1 or seq <= 1):
+        if len(n) == 1:
+            return 0
+        if len(n) == 2 and n[0] == batch and not packed:
+            return st[0]
+    raise ValueError("positions must be [batch, seq] or [seq] (one for all), [tokens] of a packed batch, with unit last "
+                     "stride")
+
+
 def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream, grad):
     if _t is None:
         _load()
@@ -161,6 +173,10 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
         if len(n) != len(shape) or n[0] != shape[0] or n[2:] != shape[2:]:
             raise ValueError("k must be shaped like q, but for the heads")
         kv = n[1]
+        if kv and not heads:
+            raise ValueError("q must have heads where k has some")
+    if not -0x80000000 <= start <= 0x7fffffff:
+        raise ValueError("start must be a 32-bit position")
     qo, ko = (None, None) if out is None else out
     if out is not None:
         if qo is None or (ko is None) != (k is None):
@@ -178,13 +194,7 @@ def _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream
     pos_stride, pos = 0, None
     if positions is not None:
         _check_int("positions", positions, dev)
-        n = positions.shape
-        if n[-1] != seq or positions.stride(-1) != 1 and seq > 1 or not (
-                len(n) == 1 or len(n) == 2 and n[0] == batch and not packed):
-            raise ValueError("positions must be [batch, seq] or [seq] (one for all), [tokens] of a packed batch, with unit "
-                             "last stride")
-        if len(n) == 2:
-            pos_stride = positions.stride(0)
+        pos_stride = _positions_of(positions, batch, seq, packed)
         pos = positions.data_ptr()
     params = _rope_arg(inv_freq, interleaved, rope_scale, dev)
     code = _code.get(dtype)

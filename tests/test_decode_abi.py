@@ -212,3 +212,20 @@ def test_frequencies():
                 dict(rot_dim=64, scaling="bands", original_len=64, low=4.0, high=4.0)):
         with pytest.raises(ValueError):
             seer.rope_freqs(**bad, device="cpu")
+
+
+@pytest.mark.parametrize("start", [2 ** 31, -2 ** 31 - 1, 2 ** 32 + 5])
+def test_binding_refuses_a_start_beyond_int32(start):
+    q = torch.zeros(1, 2, 4, 64)
+    with pytest.raises(ValueError, match="start"):
+        seer.rope(q, None, seer.rope_freqs(64, device="cpu")[0], start=start)
+
+
+def test_binding_refuses_keys_beside_no_queries():
+    with pytest.raises(ValueError, match="heads"):
+        seer.rope(torch.zeros(1, 0, 4, 64), torch.zeros(1, 2, 4, 64), seer.rope_freqs(64, device="cpu")[0])
+
+
+def test_positions_are_axes_of_tokens():
+    with pytest.raises(ValueError, match="positions"):
+        decode._positions_of(torch.tensor(3, dtype=torch.int32), 1, 1, False)
