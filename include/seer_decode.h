@@ -22,7 +22,9 @@
  * when interleaved.  Elements from rot_dim on are left as they are:
  *   x' = scale (x cos a - y sin a),  y' = scale (x sin a + y cos a)
  * Angles are reduced to a turn in 64-bit fixed point before the sine: off by 2^-52 of
- * the angle at most, less than fp32's rounding up to 2^27 radians and 5e-7 at 2^31.
+ * the angle and by 2^-64 of a turn per position at most (3.4e-19 radians; 7.3e-10 at position
+ * 2^31), less than fp32's rounding up to 2^27 radians and 5e-7 at 2^31.  Cosine and sine are
+ * within 8 steps of 2^-24 of their own size beside that, however slow the plane.
  *
  * Paged cache.  A pool of num_pages pages of page_size slots for each of K and V,
  * [page][head][slot][head_dim] with element strides given per (page, head,

@@ -1,0 +1,42 @@
+"""What the fp32 arithmetic of the generation calls keeps, on inputs that show one error alone: the
+angles of slow planes near position 0, a rotated q, the weights of the second product.
+
+u = 2^-24 is half a step of fp32 relative to the value."""
+import math
+
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+seer = pytest.importorskip("paper_2410_13276_amd")
+
+pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
+
+
+@pytest.mark.parametrize("sign", [1, -1], ids=["forward", "backward"])
+@pytest.mark.parametrize("inter", [False, True], ids=["halves", "pairs"])
+def test_slow_planes_keep_their_sine(inter, sign):
+    """One element of each plane is 1 and the other 0, so the results are the cosine and the sine themselves.
+
+    Bound, relative to the value: the rest of the angle is two conversions (u of the whole: where the words have opposite
+    signs the whole is at least half of the high one), two products with constants (2 u) and a sum (u), 5 u at most; the
+    series on it 1.5 u, the truncated terms 0.6 u, and the scale 1 and the zero element round nothing: 8 u.  Absolute: the
+    rate is held to 2^-52 of itself and 2^-64 of a turn."""
+    print(f"[precision] slow planes {inter} {sign}", flush=True)
+    f = torch.tensor([2.6e-6, 1e-6, 2.5e-7, 1e-7, 1.7e-8, 1e-8, 3e-9, 1e-9], dtype=torch.float64) * sign
+    pos = torch.tensor([1, 2, 3, 7, 100, 1000, 12345, -1, -2, -77, 1 << 20, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32)
+    first = torch.zeros(16)
+    first[0:16:2] = 1.0
+    if not inter:
+        first = torch.cat([torch.ones(8), torch.zeros(8)])
+    x = torch.zeros(1, 1, len(pos), 64)
+    x[..., :16] = first
+    y, _ = seer.rope(x.cuda(), None, f.cuda(), pos.cuda(), interleaved=inter)
+    y = y.cpu()[0, 0, :, :16].double().numpy()
+    c, s = (y[:, 0::2], y[:, 1::2]) if inter else (y[:, :8], y[:, 8:])
+    a = pos.numpy().astype(np.longdouble)[:, None] * f.numpy().astype(np.longdouble)[None, :]
+    off = np.abs(a) * 2.0 ** -52 + np.abs(pos.numpy().astype(np.longdouble))[:, None] * (2 * math.pi * 2.0 ** -64)
+    for got, want in ((s, np.sin(a)), (c, np.cos(a))):
+        over = np.abs(got - want) - (8 * U * np.abs(want) + off)
+        assert bool((over <= 0).all()), float((np.abs(got - want) / np.abs(want)).max())
