@@ -116,7 +116,7 @@ size_t seer_paged_attn_workspace_bytes(const seer_paged_desc* desc);
  * Attention over the cache: the query of token (b, s) sees the keys at positions
  * t <= positions[b][s] of table row b whose page exists,
  *   o = softmax(sm_scale q K^T) V,
- * sm_scale <= 0 selecting 1 / sqrt(head_dim).  Query head h reads KV head h / (heads_q /
+ * sm_scale (at most 2^127) <= 0 selecting 1 / sqrt(head_dim).  Query head h reads KV head h / (heads_q /
  * heads_kv).  Positions beyond the table see every key it holds.  rope (NULL: none)
  * rotates q at its position first (in fp32, not rounded).  A row that sees no
  * key (position negative, or no page) yields o = 0 and lse = -inf.  lse: device float

@@ -190,6 +190,8 @@ seer_status seer_paged_attn(const seer_paged_desc* d, const seer_rope_params* ro
       !aligned(table, 4) || !aligned(positions, 4))
     return SEER_ERR_INVALID_ARG;
   if (!std::isfinite(sm_scale)) return SEER_ERR_INVALID_ARG;
+  // (the weights are powers of 2, and an infinite sm_scale log2(e) would make the largest one 2^(0 inf))
+  if (sm_scale > 0x1p127f) return SEER_ERR_INVALID_ARG;
   if (!workspace ||
       workspace_bytes < seer::paged_attn_workspace(d->batch, d->heads_q, d->heads_kv, d->tokens, d->head_dim))
     return SEER_ERR_WORKSPACE;
