@@ -130,8 +130,10 @@ size_t seer_paged_attn_workspace_bytes(const seer_paged_desc* desc);
  * workspace: device memory of at least seer_paged_attn_workspace_bytes(desc) bytes, 256-byte
  * aligned, not shared with a call that may run at the same time.  Its contents need no set-up.
  * The cache is read once for each 32 query rows (heads_q / heads_kv x tokens).  o may not overlap an input.
- * SEER_ERR_UNSUPPORTED: as seer_kv_append, page or slot strides of 64 GB and more, more than 2^23 blocks of 16 query
- * rows (the sum over batch and heads_kv of heads_q / heads_kv x tokens / 16, each rounded up).
+ * SEER_ERR_UNSUPPORTED: head_dim not 64 or 128, a rot_dim that is no multiple of 16, strides that are no multiple of 16
+ * bytes, a table whose rows have room for more than 2^30 tokens, page or slot strides of 64 GB and more, more than 2^23
+ * query rows a KV head (heads_q / heads_kv x tokens) or 2^23 blocks of 16 of them (the sum over batch and heads_kv, each
+ * rounded up).
  */
 seer_status seer_paged_attn(const seer_paged_desc* desc, const seer_rope_params* rope, float sm_scale, const void* q,
                             const void* k_cache, const void* v_cache, const int32_t* table,

@@ -12,7 +12,7 @@ namespace {
 
 constexpr int64_t kMostTokens = (int64_t)1 << 27;    // of one rope or append call (a launch holds less than 2^32 threads)
 constexpr int64_t kMostKeys = (int64_t)1 << 30;      // of one table row
-constexpr int64_t kMostRows = (int64_t)1 << 23;      // blocks of at least 16 query rows of one KV head, of one attention call
+constexpr int64_t kMostRows = (int64_t)1 << 23;      // query rows of one KV head, and blocks of 16 of them, of one attention call
 
 bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
@@ -87,7 +87,7 @@ seer_status check_paged(const seer_paged_desc* d) {
   if (s == SEER_OK) s = check_cache_strides(d->v_cache_stride, d->dtype);
   if (s != SEER_OK) return s;
   const int64_t rows = (int64_t)d->heads_q / d->heads_kv * d->tokens;
-  const int64_t blocks = rows / 16 + 1, items = (int64_t)d->batch * d->heads_kv;
+  const int64_t blocks = (rows + 15) / 16, items = (int64_t)d->batch * d->heads_kv;
   if (rows > kMostRows || items > kMostRows || items * blocks > kMostRows) return SEER_ERR_UNSUPPORTED;
   return SEER_OK;
 }
