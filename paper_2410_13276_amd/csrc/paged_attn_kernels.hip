@@ -27,9 +27,10 @@
 // scores S^T are the very ones that its operand P^T of the second product needs.  Only Q^T is read
 // from the LDS, a tile at a time: the registers hold the tile, the accumulators and loads in flight.
 //
-// Precision: fp32 statistics and sums.  In bf16, P enters the second product in two
-// bf16 parts, and so does a q that is rotated here: the matrix cores are idle most of
-// the time (the second part of P costs nothing at 4 columns, 4 us of 56 at 28), and o is then rounded once.
+// Precision: fp32 statistics and sums.  In bf16, a q that is rotated here enters the first product in three bf16 parts,
+// which hold fp32 whole (two parts cost 0.3 us less for a token after 2000 tokens and 1.2 of 58 for four drafted ones, and left
+// the log-sum-exp of drawn cases up to 1.2e-5 off where this leaves 1.6e-6), P the second one in two: the matrix cores are
+// idle most of the time (the second part of P costs nothing at 4 columns, 4 us of 56 at 28), and o is then rounded once.
 #include <algorithm>
 
 #include "decode.h"
@@ -186,6 +187,23 @@ __device__ __forceinline__ void rotate8(const RopeView& r, const float2* cs, int
   }
 }
 
+// x as the sum of three bf16 parts, exactly: 8 significant bits of what is left each time.
+__device__ __forceinline__ void split3(const float (&x)[8], bf16x8 (&y)[3]) {
+  u32x4 z[3];
+  float rest[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) rest[e] = x[e];
+#pragma unroll
+  for (int part = 0; part < 3; ++part) {
+#pragma unroll
+    for (int f = 0; f < 4; ++f)
+      z[part][f] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * f + 1]), __float_as_uint(rest[2 * f]), 0x07060302u);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+    y[part] = __builtin_bit_cast(bf16x8, z[part]);
+  }
+}
+
 // A tile's operands as a lane holds them.
 template <typename T, int D>
 struct Tile {
@@ -227,7 +245,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   // (every line of the arguments is fetched now, not when it is first needed)
   asm volatile("" ::"s"(a.osb), "s"(a.kc.ptr), "s"(a.table.ptr), "s"(a.batch), "s"(ka.kst.page), "s"(ka.part_o));
 
-  const bool rope = QP == 2 || (!BF && a.rope.freq != nullptr);
+  const bool rope = QP == 3 || (!BF && a.rope.freq != nullptr);
   // angle per position of plane `lane` (no branch around the load: it would be waited for at once)
   const double freq = (rope ? a.rope.freq : (const double*)a.kc.ptr)[rope ? min(lane, a.rope.rot / 2 - 1) : 0];
 
@@ -395,7 +413,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
 #pragma unroll
       for (int f = 0; f < QW; ++f) {
         q_own[i][f] = *(const u32x4*)((const char*)(src + d0) + 16 * f);
-        if (QP == 2 || !BF) q_other[i][f] = *(const u32x4*)((const char*)other + 16 * f);
+        if (QP == 3 || !BF) q_other[i][f] = *(const u32x4*)((const char*)other + 16 * f);
       }
     }
     load_k(pg, key0);
@@ -430,19 +448,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
       const float2* cs = sh.cs[fast_quot(ka.group, min(r0 + rl, ka.rows - 1)) - t_first];
       if constexpr (BF) {
         const int j = d0 / 32, at = d0 % 32 / 8 * 16 + rl % 16;
-        if constexpr (QP == 2) {
+        if constexpr (QP == 3) {
           float y[8], z[8];
           unpack8(q_own[i], y);
           unpack8(q_other[i], z);
           if (turns) rotate8(a.rope, cs, d0, y, z);
-          bf16x8 hi, lo;
+          bf16x8 z3[3];
+          split3(y, z3);
 #pragma unroll
-          for (int f = 0; f < 8; ++f) {
-            hi[f] = (__bf16)y[f];
-            lo[f] = (__bf16)(y[f] - (float)hi[f]);
-          }
-          sh.q[0][rl / 16][j][at] = __builtin_bit_cast(u32x4, hi);
-          sh.q[QP - 1][rl / 16][j][at] = __builtin_bit_cast(u32x4, lo);
+          for (int part = 0; part < QP; ++part) sh.q[part][rl / 16][j][at] = __builtin_bit_cast(u32x4, z3[part]);
         } else {
           sh.q[0][rl / 16][j][at] = q_own[i][0];
         }
@@ -846,7 +860,7 @@ template <typename T, int D>
 hipError_t launch_typed(const KernelArgs& k, int nt, dim3 grid, hipStream_t s) {
   hipError_t e;
   if constexpr (sizeof(T) == 2) {
-    if (k.a.rope.freq) e = nt == 2 ? launch<T, D, 2, 2>(k, grid, s) : launch<T, D, 1, 2>(k, grid, s);
+    if (k.a.rope.freq) e = nt == 2 ? launch<T, D, 2, 3>(k, grid, s) : launch<T, D, 1, 3>(k, grid, s);
     else e = nt == 2 ? launch<T, D, 2, 1>(k, grid, s) : launch<T, D, 1, 1>(k, grid, s);
   } else {
     e = nt == 2 ? launch<T, D, 2, 1>(k, grid, s) : launch<T, D, 1, 1>(k, grid, s);

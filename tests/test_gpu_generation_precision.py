@@ -40,3 +40,41 @@ def test_slow_planes_keep_their_sine(inter, sign):
     for got, want in ((s, np.sin(a)), (c, np.cos(a))):
         over = np.abs(got - want) - (8 * U * np.abs(want) + off)
         assert bool((over <= 0).all()), float((np.abs(got - want) / np.abs(want)).max())
+
+
+def _one_key(b, wide):
+    """A table of b sequences of pages of one slot, sequence i having page i at position i alone."""
+    table = torch.full((b, wide), -1, dtype=torch.int32)
+    table[torch.arange(b), torch.arange(b)] = torch.arange(b, dtype=torch.int32)
+    return table
+
+
+@pytest.mark.parametrize("tokens", [1, 2])
+@pytest.mark.parametrize("heads", [8, 32], ids=["one column tile", "two"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_rotated_q_is_not_rounded(dtype, D, heads, tokens):
+    """One key, q of one plane (a, 0) a head: lse = sm_scale a cos(p f) k, all else zero.
+
+    Bound, relative: the cosine 8 u (test_slow_planes_keep_their_sine), its product with a u, what is left of three products
+    with k in a sum 3 u, log2(e) and the score u + 0.3 u, ln 2 and the product with it u + 0.1 u (the sum of the weights is 1,
+    its logarithm 0): 15 u.  A q in 16 bits is up to 64 u off."""
+    print(f"[precision] rotated q {dtype} {D} {heads} {tokens}", flush=True)
+    gen = torch.Generator().manual_seed(D + heads)
+    B, n = 48, D // 2
+    a = (1 + torch.rand(B, heads, tokens, generator=gen)).to(dtype)
+    plane = torch.arange(heads) % n
+    q = torch.zeros(B, heads, tokens, D, dtype=dtype)
+    q[:, torch.arange(heads), :, plane] = a.transpose(0, 1)
+    kc = torch.zeros(B, 1, 1, D, dtype=dtype)
+    kc[..., :n] = 2.0
+    f = torch.tensor([10000.0 ** (-2 * p / D) for p in range(n)], dtype=torch.float64)
+    pos = torch.arange(B, dtype=torch.int32)[:, None] + torch.tensor([0, 5])[:tokens].to(torch.int32)
+    _, lse = seer.paged_attn(q.cuda(), kc.cuda(), kc.cuda(), _one_key(B, B + 8).cuda(), pos.cuda(), inv_freq=f.cuda(),
+                             sm_scale=0.25, want_lse=True)
+    c = np.cos(pos.numpy().astype(np.longdouble)[:, None, :] * f.numpy().astype(np.longdouble)[plane.numpy()][None, :, None])
+    want = 0.5 * a.double().numpy() * c
+    off = np.abs(lse.cpu().double().numpy() - want)
+    at = pos.numpy().astype(np.longdouble)[:, None, :]  # 2^-52 of the angle and 2^-64 of a turn a position, times the slope
+    bound = 15 * U * np.abs(want) + 0.5 * a.double().numpy() * at * (2.0 ** -52 + 2.0 ** -61)
+    assert bool((off <= bound).all()), float((off / np.abs(want)).max() / U)
