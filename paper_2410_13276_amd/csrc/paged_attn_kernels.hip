@@ -27,10 +27,11 @@
 // scores S^T are the very ones that its operand P^T of the second product needs.  Only Q^T is read
 // from the LDS, a tile at a time: the registers hold the tile, the accumulators and loads in flight.
 //
-// Precision: fp32 statistics and sums.  In bf16, a q that is rotated here enters the first product in three bf16 parts,
-// which hold fp32 whole (two parts cost 0.3 us less for a token after 2000 tokens and 1.2 of 58 for four drafted ones, and left
-// the log-sum-exp of drawn cases up to 1.2e-5 off where this leaves 1.6e-6), P the second one in two: the matrix cores are
-// idle most of the time (the second part of P costs nothing at 4 columns, 4 us of 56 at 28), and o is then rounded once.
+// Precision: fp32 statistics and sums.  In bf16, P enters the second product in three bf16 parts, which hold fp32 whole, and
+// so does a q that is rotated here the first; o is then rounded once.  The matrix cores are idle most of the time: two parts
+// of q cost 0.3 us less for a token after 2000 tokens and 1.2 of 58 for four drafted ones, and left the log-sum-exp up to
+// 1.2e-5 off where this leaves 1.5e-6; two of P cost 0.2 us and 1.3 of 51 less, and gave 0.08 to 0.2% of o's elements
+// another last bit than the same formula wholly in fp32 does, where this gives at most 0.07%.
 #include <algorithm>
 
 #include "decode.h"
@@ -553,19 +554,15 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
       }
     };
 
-    // P^T as the operand of the second product (bf16: in two parts)
+    // P^T as the operand of the second product (bf16: in three parts, fp32 whole)
     struct Weights {
-      bf16x8 hi, lo;
+      bf16x8 part[3];
       float p[S::PK];
     };
     auto weights = [&](const float (&p)[S::PK]) -> Weights {
       Weights w;
       if constexpr (BF) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          w.hi[e] = (__bf16)p[e];
-          w.lo[e] = (__bf16)(p[e] - (float)w.hi[e]);
-        }
+        split3(p, w.part);
       } else {
 #pragma unroll
         for (int e = 0; e < S::PK; ++e) w.p[e] = p[e];
@@ -574,15 +571,16 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
     };
     // y + V^T P^T of accumulator i, the bits outside `keep` taken as 0.  Element f of the
     // lane: column n, feature (4 g + f) D / 16 + i (bf16), 64 (i / 4) + 4 (4 g + f) + i % 4 (fp32)
-    auto product = [&](const Weights& w, int i, f32x4 y, const uint32_t (&keep)[4]) -> f32x4 {
+    auto product = [&](const Weights& w, int i, f32x4 y, const uint32_t (&keep)[4], const uint32_t (&take)[2]) -> f32x4 {
       if constexpr (BF) {
         u32x4 z;
 #pragma unroll
         for (int f = 0; f < 4; ++f)
-          z[f] = keep[f] & __builtin_amdgcn_perm(t.v[2 * f + 1][i / 2], t.v[2 * f][i / 2], i % 2 ? 0x07060302u : 0x05040100u);
+          z[f] = keep[f] & __builtin_amdgcn_perm(t.v[2 * f + 1][i / 2], t.v[2 * f][i / 2], take[i % 2]);
         const bf16x8 vt = __builtin_bit_cast(bf16x8, z);
-        y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w.lo, y, 0, 0, 0);
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w.hi, y, 0, 0, 0);
+#pragma unroll
+        for (int part = 2; part >= 0; --part) y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, w.part[part], y, 0, 0, 0);
+        return y;
       } else {
 #pragma unroll
         for (int e = 0; e < S::PK; ++e)
@@ -590,6 +588,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
         return y;
       }
     };
+
+    constexpr uint32_t kTake[2] = {0x05040100u, 0x07060302u};  // the low and the high halves of two dwords
 
     // the bits of V's operands that belong to the keys in `seen`
     auto mask = [&](uint32_t seen, uint32_t (&keep)[4]) {
@@ -627,7 +627,7 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
 #pragma unroll
       for (int i = 0; i < NA; ++i)
 #pragma unroll
-        for (int ct = 0; ct < NT; ++ct) acc[ct][i] = product(w[ct], i, acc[ct][i], keep);
+        for (int ct = 0; ct < NT; ++ct) acc[ct][i] = product(w[ct], i, acc[ct][i], keep, kTake);
       __builtin_amdgcn_sched_barrier(0);  // (as above, for V)
       load_v(pg, key0 + STEP);
     }
@@ -650,10 +650,12 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
           const uint32_t seen = t.there & ((1u << min(max(end - lane_key, 0), S::PK)) - 1u);
           uint32_t keep[4];
           mask(seen, keep);
+          uint32_t take[2] = {kTake[0], kTake[1]};
+          asm volatile("" : "+s"(take[0]), "+s"(take[1]));  // (V is transposed here each time: kept for all tokens, it would spill)
 #pragma unroll
           for (int i = 0; i < NA; ++i) {
             __builtin_amdgcn_sched_barrier(0);  // (one at a time: side by side they would spill)
-            const f32x4 o = product(w, i, f32x4{0.f, 0.f, 0.f, 0.f}, keep);
+            const f32x4 o = product(w, i, f32x4{0.f, 0.f, 0.f, 0.f}, keep, take);
             if (token[ct] == tk) acc[ct][i] += o;
           }
         }

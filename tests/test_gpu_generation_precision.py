@@ -78,3 +78,47 @@ def test_rotated_q_is_not_rounded(dtype, D, heads, tokens):
     at = pos.numpy().astype(np.longdouble)[:, None, :]  # 2^-52 of the angle and 2^-64 of a turn a position, times the slope
     bound = 15 * U * np.abs(want) + 0.5 * a.double().numpy() * at * (2.0 ** -52 + 2.0 ** -61)
     assert bool((off <= bound).all()), float((off / np.abs(want)).max() / U)
+
+
+def _parts(p):
+    """p (longdouble) to the nearest bf16, and what is left of it to the nearest bf16."""
+    hi = torch.from_numpy(p.astype(np.float64)).bfloat16()
+    lo = torch.from_numpy((p - hi.double().numpy().astype(np.longdouble)).astype(np.float64)).bfloat16()
+    return hi, lo
+
+
+@pytest.mark.parametrize("tokens", [1, 2])
+@pytest.mark.parametrize("heads", [1, 20], ids=["one column tile", "two"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=["bf16", "f32"])
+def test_weights_are_not_rounded(dtype, D, heads, tokens):
+    """Keys of weights 1, p and 1 whose values are the first 8 bits of p, -1 and the next 8: o (2 + p) is what 16 bits leave
+    of p.  Two tokens see different keys (the fourth has no weight), which takes the path of the keys near new tokens.
+
+    Bound of o (2 + p): p's exponent, below 1.35, is off by u and 0.2 u of itself, so p by 0.9 u, and by 2 u in its exp2:
+    3 u p.  The sums of the products are exact: all terms are multiples of 2^-25 and below 1 together.  The sum of the
+    weights, its inverse and the product round o by 4 u of itself, the output by half a step.  A p in 16 bits leaves o = 0."""
+    print(f"[precision] weights {dtype} {D} {heads} {tokens}", flush=True)
+    B = 90
+    x = (torch.arange(B) + 30).double() / 128  # the scores are 0, -x, 0: p from 0.39 to 0.79
+    x = x[x < 0.95]
+    B = len(x)
+    p = np.exp(-x.numpy().astype(np.longdouble))
+    hi, lo = _parts(p)
+    left = hi.double().numpy().astype(np.longdouble) + lo.double().numpy() - p
+    assert float(np.abs(left).max()) > 12 * U  # (the inputs show it)
+    kc, vc = torch.zeros(B, 1, 4, D, dtype=dtype), torch.zeros(B, 1, 4, D, dtype=dtype)
+    kc[:, 0, 1, 0] = -x.to(dtype)
+    kc[:, 0, 3, 0] = -1e4
+    assert torch.equal(kc[:, 0, 1, 0].double(), -x)
+    vc[:, 0, 0], vc[:, 0, 1], vc[:, 0, 2] = hi.to(dtype)[:, None], -1.0, lo.to(dtype)[:, None]
+    q = torch.zeros(B, heads, tokens, D, dtype=dtype)
+    q[..., 0] = 1.0
+    table = torch.arange(B, dtype=torch.int32)[:, None]
+    pos = torch.tensor([[2, 3]], dtype=torch.int32).expand(B, 2)[:, :tokens].contiguous()
+    o, _ = seer.paged_attn(q.cuda(), kc.cuda(), vc.cuda(), table.cuda(), pos.cuda(), sm_scale=1.0)
+    want = (left / (2 + p))[:, None, None, None]
+    half = 2.0 ** -8 if dtype == torch.bfloat16 else U
+    bound = (3 * U * p / (2 + p))[:, None, None, None] * (1 + half) + (4 * U + half) * np.abs(want)
+    off = np.abs(o.cpu().double().numpy() - want)
+    assert bool((off <= bound).all()), float((off * 2.8).max() / U)
