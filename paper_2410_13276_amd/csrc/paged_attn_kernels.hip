@@ -225,6 +225,10 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   constexpr int kRowCost = NT;
   constexpr int OSTR = D + 4;
   constexpr int QJ = BF ? D / 32 : D / 16;
+  // Partial sums of an fp32 score, joined by pairs: one chain of D sums rounds off twice as far (o of 1000 keys on average
+  // 5.2e-7 off, with two sums 3.1e-7, with four 2.6e-7).  Beside two column tiles of 128 features four of them spill (28 / 4
+  // heads, four tokens: 94.7 us, with two sums 92.6, with one 92.9; 24 / 1 heads 41.8, 39.7 and 40.0).
+  constexpr int SUMS = BF ? 1 : NT == 2 && D == 128 ? 2 : 4;
   // the operand Q^T as the lanes read it and the tokens' cosines and sines, then the wavefronts' results
   __shared__ union {
     struct {
@@ -502,9 +506,9 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
 
     // S^T of a column tile: element e is key key0 + PK g + e of the lane's column
     auto scores = [&](int ct, int at, float (&s)[S::PK]) {
-      f32x4 y[S::KSUB];
+      f32x4 y[S::KSUB * SUMS];
 #pragma unroll
-      for (int i = 0; i < S::KSUB; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < S::KSUB * SUMS; ++i) y[i] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int part = QP - 1; part >= 0; --part)
 #pragma unroll
@@ -518,11 +522,13 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
             } else {
 #pragma unroll
               for (int f = 0; f < 4; ++f)
-                y[i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][f]), __uint_as_float(q[f]), y[i],
-                                                            0, 0, 0);
+                y[f % SUMS] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(t.k[i][j][f]), __uint_as_float(q[f]),
+                                                                   y[f % SUMS], 0, 0, 0);
             }
           }
         }
+      if constexpr (SUMS == 4) y[0] = (y[0] + y[1]) + (y[2] + y[3]);
+      if constexpr (SUMS == 2) y[0] += y[1];
 #pragma unroll
       for (int i = 0; i < S::KSUB; ++i)
 #pragma unroll

@@ -122,3 +122,32 @@ def test_weights_are_not_rounded(dtype, D, heads, tokens):
     bound = (3 * U * p / (2 + p))[:, None, None, None] * (1 + half) + (4 * U + half) * np.abs(want)
     off = np.abs(o.cpu().double().numpy() - want)
     assert bool((off <= bound).all()), float((off * 2.8).max() / U)
+
+
+@pytest.mark.parametrize("heads", [1, 20], ids=["one column tile", "two"])
+@pytest.mark.parametrize("D", [64, 128])
+def test_fp32_scores_are_sums_of_short_chains(D, heads):
+    """One key of ones and q of D equal values, chosen so that one chain of D sums rounds the same way at most of its steps
+    (by up to D / 4 u in the end): lse = sm_scale D c.
+
+    Bound, relative: a chain of n sums of c is off by u (c + 2 c + .. + n c), that is u n (n + 1) / 2 of c, 4 of them (2 in
+    blocks of more than 16 rows of 128) with n = D / 4 (D / 2); putting them together by pairs rounds D once or twice.  To
+    that log2(e), the score, ln 2 and the product with it: 2.3 u (test_rotated_q_is_not_rounded)."""
+    print(f"[precision] chains {D} {heads}", flush=True)
+    c = (1 + np.random.default_rng(D).random(20000)).astype(np.float32)
+    chain = np.zeros_like(c)
+    for _ in range(D):
+        chain = chain + c
+    off = np.abs(chain.astype(np.float64) - D * c.astype(np.float64)) / (D * c.astype(np.float64)) / U
+    c = torch.from_numpy(c[np.argsort(off)[-40:]])
+    assert float(np.sort(off)[-40]) > D / 4 - 4
+    q = c[:, None, None, None].expand(40, heads, 1, D).contiguous()
+    kc = torch.ones(1, 1, 1, D)
+    table = torch.zeros(40, 1, dtype=torch.int32)
+    _, lse = seer.paged_attn(q.cuda(), kc.cuda(), kc.cuda(), table.cuda(), table.cuda(), sm_scale=0.125, want_lse=True)
+    want = 0.125 * D * c.double()[:, None, None]
+    sums = 2 if D == 128 and heads > 16 else 4
+    n = D // sums
+    bound = (sums * n * (n + 1) / 2 + D * math.log2(sums)) / D + 2.3
+    worst = float(((lse.cpu().double() - want).abs() / want).max()) / U
+    assert worst <= bound, worst
