@@ -116,20 +116,29 @@ size_t seer_paged_attn_workspace_bytes(const seer_paged_desc* desc);
  * Attention over the cache: the query of token (b, s) sees the keys at positions
  * t <= positions[b][s] of table row b whose page exists,
  *   o = softmax(sm_scale q K^T) V,
- * sm_scale (at most 2^127) <= 0 selecting 1 / sqrt(head_dim).  Query head h reads KV head h / (heads_q /
+ * sm_scale at most 2^127, a value <= 0 selecting 1 / sqrt(head_dim).  Query head h reads KV head h / (heads_q /
  * heads_kv).  Positions beyond the table see every key it holds.  rope (NULL: none)
  * rotates q at its position first (in fp32, not rounded).  A row that sees no
  * key (position negative, or no page) yields o = 0 and lse = -inf.  lse: device float
  * [batch][heads_q][tokens], natural log, or NULL.  What unseen slots hold has no
- * effect on the results, be it NaN.
+ * effect on the results, be it NaN.  Statistics, weights and sums are fp32, o is rounded once.  Seen values
+ * that are not finite make o of the rows that see them NaN or infinite, whatever their weights, and so do seen keys
+ * the rows whose q is rotated here.
  *
  * The work, sequences of any lengths, is cut evenly over the workgroups: one sequence's keys
- * may be split over many of them, whose partial results a second launch joins.
+ * may be split over many of them, whose partial results a second launch joins.  Whether there is one goes by the room of a
+ * table row, not by the lengths, which only the device knows: beyond 512 keys (fp32: 256), and beyond twice that with 128
+ * to 512 KV heads in the batch (blocks of 32 query rows counted each).  It costs 2 to 4 us; a caller whose sequences are all
+ * short avoids it by giving fewer max_pages with the same table_stride.
  * Results are the same bit for bit from run to run; they may differ by fp32 rounding
  * from those of the same sequence in another batch (the cuts lie elsewhere).
  * workspace: device memory of at least seer_paged_attn_workspace_bytes(desc) bytes, 256-byte
  * aligned, not shared with a call that may run at the same time.  Its contents need no set-up.
- * The cache is read once for each 32 query rows (heads_q / heads_kv x tokens).  o may not overlap an input.
+ * The cache is read once for each 32 query rows (heads_q / heads_kv x tokens), and the positions of a sequence one after
+ * the other: made for one token or a few.  Any number up to the limits below gives right results, at a rate that falls
+ * behind a matrix product's (32 / 8 heads of 128, bf16, after 16000 tokens: 512 tokens take 0.38 ms, 2048 2.4 ms, 3 to 5
+ * times what their products need); a whole prompt goes through seer_bsattn or seer_dense_attn before its keys are
+ * appended.  o may not overlap an input.
  * SEER_ERR_UNSUPPORTED: head_dim not 64 or 128, a rot_dim that is no multiple of 16, strides that are no multiple of 16
  * bytes, a table whose rows have room for more than 2^30 tokens, page or slot strides of 64 GB and more, more than 2^23
  * query rows a KV head (heads_q / heads_kv x tokens) or 2^23 blocks of 16 of them (the sum over batch and heads_kv, each

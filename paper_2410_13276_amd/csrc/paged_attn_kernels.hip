@@ -4,10 +4,10 @@
 // G = heads_q / heads_kv heads (times the tokens, where a few drafted ones come
 // together) are the columns of one matrix product with the cache: S^T = K Q^T,
 // O^T = V^T P^T.  That is at most 2 * 32 operations a cached element, far below
-// what the matrix cores do in the time HBM takes to bring it (they are busy 7% of the time with 4
+// what the matrix cores do in the time HBM takes to bring it (they are busy 11% of the time with 4
 // columns): the kernel is bound by reading K and V once, and everything else is arranged around
 // that.  A token after 131072 tokens (32 / 8 heads of 128, bf16) reads 537 MB in 93 us, 64 sequences of 200 to 16000
-// tokens 955 MB in 168 us (5.8 and 5.7 TB/s; a kernel that only reads takes 87 and 159 us, a copy moves 5.1 TB/s).
+// tokens 955 MB in 169 us (5.8 and 5.7 TB/s; a kernel that only reads takes 87 and 159 us, a copy moves 5.1 TB/s).
 // Without any of the arithmetic the first takes 1% less.
 //
 // Work.  The keys of every (sequence, KV head) are cut into units of a tile for each
@@ -45,8 +45,8 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kWorkers = 512;   // workgroups at most: two for each CU
 // Rows are not split, and the second launch not made, where a row has room for so many keys at most (fp32: half), and
 // for twice as many where 128 rows or more, but not more than workgroups, share the launch.  Whole against split, 32 / 8
-// heads of 128: 1 sequence of 400 tokens 9.7 and 11.2 us, of 900 14.2 and 11.4; 16 of 900 16.0 and 18.9; 64 of 900 47.3 and
-// 48.6; fp32, 8 / 8 heads of 64, 1 of 400 10.9 and 9.3, 64 of 400 20.5 and 22.5.
+// heads of 128: 1 sequence of 400 tokens 10.7 and 11.9 us, of 900 15.3 and 11.9; 16 of 900 17.1 and 19.3; 64 of 900 47.5 and
+// 49.5; fp32, 8 / 8 heads of 64, 1 of 400 11.0 and 9.3, 64 of 400 20.9 and 22.7.
 constexpr int kWholeKeys = 512;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -220,8 +220,8 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   constexpr bool BF = sizeof(T) == 2;
   constexpr int NA = D / 16;          // accumulators of a column tile
   constexpr int ROWS = 16 * NT;
-  // A row's beginning and end, in units: what it weighs beside its units (64 sequences of 200 to 16000 tokens: 189 us
-  // without, 180 with 1, 181 with 2; four drafted tokens on two column tiles: 61.3, 56.0, 55.0)
+  // A row's beginning and end, in units: what it weighs beside its units (64 sequences of 200 to 16000 tokens: 186 us
+  // without, 177 with 1, 181 with 2; four drafted tokens on two column tiles: 55.0, 50.6, 50.4)
   constexpr int kRowCost = NT;
   constexpr int OSTR = D + 4;
   constexpr int QJ = BF ? D / 32 : D / 16;

@@ -3,12 +3,12 @@
 //
 // Both move memory: a read and a write of every element, and some 10 operations on
 // it.  A thread owns two 16-byte pieces of one token's heads (8 planes in bf16, 4 in fp32), forms their
-// cosines and sines once and walks over up to 8 heads with them, so that the angles (about 30
-// instructions a plane) are shared and every access is 16 bytes.  No table of cosines is read: the angle is an
+// cosines and sines once and walks over up to 8 heads with them, so that the angles (about 50
+// instructions a plane, its rate's among them) are shared and every access is 16 bytes.  No table of cosines is read: the angle is an
 // integer product of the position and the plane's turn rate (decode.h).  Large calls run at a copy's rate (5.1 TB/s of
 // reads and writes): 32768 tokens of 32 + 8 heads of 128 in bf16, 671 MB, take 123 us (5.4 TB/s); 25000 tokens of 20 prompts
-// with 8 KV heads into pages, 206 MB, 33 us by the kernel trace (repeated passes, which may find data in the last-level cache), 39 a
-// pass among others.  Small ones take 3 to 4 us, in which little more than loads that wait for each other (position, table
+// with 8 KV heads into pages, 206 MB, 33 us by the kernel trace (repeated passes, which may find data in the last-level cache), 40 a
+// pass among others.  Small ones take 3.5 to 4.3 us, in which little more than loads that wait for each other (position, table
 // entry, data) happens.
 #include <algorithm>
 

@@ -10,7 +10,8 @@ cache, and attention of new tokens over it.  Re-exported by the package.
         o, _ = seer.paged_attn(q1, kc, vc, table, positions, inv_freq=freqs)
 
 Tensors of a call are on one GPU, which need not be the current one; work runs on
-that GPU's current stream unless `stream` is given.
+that GPU's current stream unless `stream` is given.  As with the package's other calls, results
+carry no autograd graph: a training program calls rope_grad in the backward pass of a function of its own.
 """
 from __future__ import annotations
 
@@ -221,7 +222,7 @@ def rope(q, k, inv_freq, positions=None, *, start: int = 0, interleaved: bool = 
          out=None, stream=None):
     """Rotary positions (seer_rope) of q and k (None: q alone), [B, H, S, D] or packed [T, H, D].  positions: int32 [B,
     S], or [S] for every batch entry ([T] packed); None: start + s.  out: (q', k') to write to, which may be (q, k).
-    Returns (q', k' or None)."""
+    Returns (q', k' or None), which carry no autograd graph: rope_grad is the way back."""
     return _rope(q, k, inv_freq, positions, start, interleaved, rope_scale, out, stream, 0)
 
 
@@ -335,8 +336,9 @@ def paged_attn(q, k_cache, v_cache, table, positions, *, inv_freq=None, interlea
                workspace=None, stream=None):
     """Attention of new tokens over the paged cache (seer_paged_attn).  q: [B, Hq, S, D], or [B, Hq, D] for one token of
     each sequence; positions: int32 [B, S] ([B]): a token sees the keys up to its own position, none where that is
-    negative.  inv_freq: q is rotated at its position first.  A workspace given by the caller must not serve two calls
-    that may run at the same time.  Returns (O, LSE [B, Hq, S] ([B, Hq]) or None)."""
+    negative.  inv_freq: q is rotated at its position first.  A table much wider than the sequences need costs short ones a
+    second launch: table[:, :n] avoids it.  A workspace given by the caller must not serve two calls that may run at the
+    same time.  Returns (O, LSE [B, Hq, S] ([B, Hq]) or None)."""
     if _t is None:
         _load()
     shape, qs = _tokens_of(q, "q")
