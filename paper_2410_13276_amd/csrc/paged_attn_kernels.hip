@@ -35,6 +35,8 @@
 #include <algorithm>
 
 #include "decode.h"
+#include "paged_common.h"
+#include "paged_join.h"
 
 namespace seer {
 
@@ -42,17 +44,11 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kWorkers = 512;   // workgroups at most: two for each CU
 // Rows are not split, and the second launch not made, where a row has room for so many keys at most (fp32: half), and
 // for twice as many where 128 rows or more, but not more than workgroups, share the launch.  Whole against split, 32 / 8
 // heads of 128: 1 sequence of 400 tokens 10.7 and 11.9 us, of 900 15.3 and 11.9; 16 of 900 17.1 and 19.3; 64 of 900 47.5 and
 // 49.5; fp32, 8 / 8 heads of 64, 1 of 400 11.0 and 9.3, 64 of 400 20.9 and 22.7.
 constexpr int kWholeKeys = 512;
-constexpr float kLn2 = 0.6931471805599453f;
-
-struct Stride16 {
-  uint32_t page, slot;
-};
 
 struct KernelArgs {
   PagedArgs a;
@@ -93,116 +89,6 @@ __device__ __forceinline__ int length_of(const KernelArgs& k, int b) {
 }
 __device__ __forceinline__ int units_of(const KernelArgs& k, int len) {
   return max(1, (len + (1 << k.unit_shift) - 1) >> k.unit_shift);
-}
-
-// The weights dealt to the workgroups: workgroup w has base (+ 1 for the first `rest`).  (All below 2^30: the
-// 64-bit divisions that this was first written with were 600 instructions at every workgroup's start.)
-struct Deal {
-  uint32_t base, rest, workers;
-  __device__ __forceinline__ Deal(uint32_t total, uint32_t groups) {
-    workers = min(groups, total);
-    base = total / workers;
-    rest = total - base * workers;
-  }
-  __device__ __forceinline__ int first(uint32_t w) const { return (int)(w * base + min(w, rest)); }
-  __device__ __forceinline__ int owner(uint32_t x) const {
-    const uint32_t big = rest * (base + 1);
-    return (int)(x < big ? x / (base + 1) : rest + (x - big) / base);
-  }
-};
-
-// Within a wavefront, without the LDS: inclusive prefix sum; least of a row of 16 lanes; largest and sum of the
-// lanes l % 16.
-template <int CTRL, int ROWS = 0xf>
-__device__ __forceinline__ int dpp(int old, int x) {
-  return __builtin_amdgcn_update_dpp(old, x, CTRL, ROWS, 0xf, false);
-}
-__device__ __forceinline__ int wave_prefix(int x) {
-  x += dpp<0x111>(0, x);  // row_shr 1, 2, 4, 8
-  x += dpp<0x112>(0, x);
-  x += dpp<0x114>(0, x);
-  x += dpp<0x118>(0, x);
-  x += dpp<0x142, 0xa>(0, x);  // row_bcast 15 to rows 1 and 3
-  x += dpp<0x143, 0xc>(0, x);  // row_bcast 31 to rows 2 and 3
-  return x;
-}
-__device__ __forceinline__ int row_min(int x) {
-  x = min(x, dpp<0xb1>(x, x));   // quad_perm 1 0 3 2
-  x = min(x, dpp<0x4e>(x, x));   // quad_perm 2 3 0 1
-  x = min(x, dpp<0x141>(x, x));  // row_half_mirror
-  return min(x, dpp<0x140>(x, x));  // row_mirror
-}
-typedef __attribute__((ext_vector_type(2))) unsigned int u32pair;
-__device__ __forceinline__ void across(float x, bool half, float& y, float& z) {
-  const uint32_t u = __float_as_uint(x);
-  const u32pair p = half ? __builtin_bit_cast(u32pair, __builtin_amdgcn_permlane32_swap(u, u, false, false))
-                         : __builtin_bit_cast(u32pair, __builtin_amdgcn_permlane16_swap(u, u, false, false));
-  y = __uint_as_float(p[0]);
-  z = __uint_as_float(p[1]);
-}
-__device__ __forceinline__ float column_max(float x) {
-  float y, z;
-  across(x, false, y, z);
-  x = fmaxf(y, z);
-  across(x, true, y, z);
-  return fmaxf(y, z);
-}
-__device__ __forceinline__ float column_sum(float x) {
-  float y, z;
-  across(x, false, y, z);
-  x = y + z;
-  across(x, true, y, z);
-  return y + z;
-}
-
-__device__ __forceinline__ void unpack8(const u32x4 (&q)[1], float (&y)[8]) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    y[2 * i] = __uint_as_float(q[0][i] << 16);
-    y[2 * i + 1] = __uint_as_float(q[0][i] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void unpack8(const u32x4 (&q)[2], float (&y)[8]) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) y[i] = __uint_as_float(q[i / 4][i % 4]);
-}
-
-// Elements d0 .. d0 + 7 of a head, y, rotated; z: the other half of their planes (half layout), cs: cosine and sine of the
-// token's planes.
-__device__ __forceinline__ void rotate8(const RopeView& r, const float2* cs, int d0, float (&y)[8], const float (&z)[8]) {
-  if (r.interleaved) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 f = cs[d0 / 2 + i];
-      const float u = y[2 * i], v = y[2 * i + 1];
-      y[2 * i] = u * f.x - v * f.y;
-      y[2 * i + 1] = u * f.y + v * f.x;
-    }
-  } else {
-    const bool second = d0 >= r.rot / 2;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float2 f = cs[(second ? d0 - r.rot / 2 : d0) + i];
-      y[i] = y[i] * f.x + z[i] * (second ? f.y : -f.y);
-    }
-  }
-}
-
-// x as the sum of three bf16 parts, exactly: 8 significant bits of what is left each time.
-__device__ __forceinline__ void split3(const float (&x)[8], bf16x8 (&y)[3]) {
-  u32x4 z[3];
-  float rest[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) rest[e] = x[e];
-#pragma unroll
-  for (int part = 0; part < 3; ++part) {
-#pragma unroll
-    for (int f = 0; f < 4; ++f)
-      z[part][f] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * f + 1]), __float_as_uint(rest[2 * f]), 0x07060302u);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
-    y[part] = __builtin_bit_cast(bf16x8, z[part]);
-  }
 }
 
 // A tile's operands as a lane holds them.
@@ -758,88 +644,6 @@ __global__ __launch_bounds__(kThreads, 2) void paged_attn_kernel(KernelArgs ka) 
   }
 }
 
-// Rows whose keys several workgroups shared: their partial results, in the order of the keys.  A workgroup joins JR
-// rows of an item, a wavefront forming the weights of a row (or part of one: all four then form the same); a thread sums
-// 4 features over the parts grp, grp + GRP, ..  Four rows a workgroup keep a large batch's launch short, one row leaves
-// fewer parts to each thread where the call has few rows (a token after 131072 tokens, 32 rows of 64 parts: 6.9 -> 4.8 us).
-constexpr int kJoinThreads = 256;
-template <typename T, int D, int JR>
-__global__ __launch_bounds__(kJoinThreads) void paged_join_kernel(KernelArgs ka, int rows_block) {
-  constexpr int V4 = D / 4, GRP = kJoinThreads / (V4 * JR), AHEAD = 8, OWN = kWorkers / kWave;
-  __shared__ float sW[JR][kWorkers];
-  __shared__ float2 sT[JR];
-  __shared__ __attribute__((aligned(16))) float sO[GRP][JR][D];
-  const PagedArgs& a = ka.a;
-  asm volatile("" ::"s"(a.osb), "s"(a.lse), "s"(a.batch), "s"(ka.rows), "s"(ka.part_o));  // (as in the kernel before)
-  const int2 rec = ka.record[blockIdx.x];
-  if (rec.x < 0) return;
-  const int items = a.heads_kv * ka.row_blocks;
-  const int b = blockIdx.x / (uint32_t)items, item = blockIdx.x - b * items;
-  const int h = fast_quot(ka.blocks, item), rb = item - h * ka.row_blocks;
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int nrows = min(rows_block, ka.rows - rb * rows_block);
-  const int w0 = rec.x / 2, parts = rec.y - w0 + 1;
-  auto slot = [&](int p, int rl) { return (int64_t)(p == 0 ? rec.x : 2 * (w0 + p)) * rows_block + rl; };
-  const float c = ka.scale_log2;
-
-  // the first parts are on their way while the weights are formed
-  const int wrow = wave % JR;
-  const int row = min((int)blockIdx.y * JR + wrow, nrows - 1);
-  float2 ml[OWN];
-#pragma unroll
-  for (int i = 0; i < OWN; ++i)
-    if (i * kWave < parts) ml[i] = ka.part_ml[slot(min(lane + i * kWave, parts - 1), row)];
-  const int d = tid % V4 * 4, jr = tid / V4 % JR, grp = tid / (V4 * JR);
-  const int rl = min((int)blockIdx.y * JR + jr, nrows - 1);
-  auto part = [&](int p) { return *(const f32x4*)(ka.part_o + slot(p, rl) * D + d); };
-  f32x4 y[AHEAD];
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i) y[i] = part(min(grp + i * GRP, parts - 1));
-
-  float mx = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < OWN; ++i)
-    if (i * kWave < parts) mx = fmaxf(mx, ml[i].x);
-  mx = wave_max(mx);
-  float sum = 0.f;
-#pragma unroll
-  for (int i = 0; i < OWN; ++i)
-    if (lane + i * kWave < parts) {
-      const float wgt = ml[i].x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((ml[i].x - mx) * c);
-      if (wave < JR) sW[wrow][lane + i * kWave] = wgt;
-      sum += wgt * ml[i].y;
-    }
-  sum = wave_sum(sum);
-  if (lane == 0 && wave < JR) sT[wrow] = make_float2(mx, sum);
-  __syncthreads();
-
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int i = 0; i < AHEAD; ++i)
-    if (grp + i * GRP < parts) o += sW[jr][grp + i * GRP] * y[i];
-#pragma unroll 4
-  for (int p = grp + AHEAD * GRP; p < parts; p += GRP) o += sW[jr][p] * part(p);
-  *(f32x4*)&sO[grp][jr][d] = o;
-  __syncthreads();
-  if (grp != 0 || (int)blockIdx.y * JR + jr >= nrows) return;
-#pragma unroll
-  for (int i = 1; i < GRP; ++i) o += *(const f32x4*)&sO[i][jr][d];
-  mx = sT[jr].x;
-  sum = sT[jr].y;
-  const int r = rb * rows_block + rl, t = fast_quot(ka.group, r), hq = h * ka.group.d + (r - t * ka.group.d);
-  const bool none = sum == 0.f;
-  T* out = (T*)a.o + b * a.osb + hq * a.osh + t * a.oss + d;
-#pragma unroll
-  for (int f = 0; f < 4; ++f) {
-    const float z = none ? 0.f : o[f] / sum;
-    if constexpr (sizeof(T) == 2) ((__bf16*)out)[f] = (__bf16)z;
-    else out[f] = z;
-  }
-  if (a.lse != nullptr && d == 0)
-    a.lse[((int64_t)b * a.heads_q + hq) * a.tokens + t] =
-        none ? -INFINITY : ((mx == -INFINITY ? 0.f : mx * c) + __log2f(sum)) * kLn2;
-}
-
 struct Plan {
   int group, rows, nt, row_blocks;
   size_t ml, o, total;  // byte offsets in the workspace (the records come first)
@@ -874,13 +678,8 @@ hipError_t launch_typed(const KernelArgs& k, int nt, dim3 grid, hipStream_t s) {
     e = nt == 2 ? launch<T, D, 2, 1>(k, grid, s) : launch<T, D, 1, 1>(k, grid, s);
   }
   if (e != hipSuccess || !k.join) return e;
-  const int64_t all = (int64_t)k.a.batch * k.a.heads_kv * k.row_blocks;
-  const int rows = std::min(k.rows, 16 * nt);
-  if (all * rows <= 2 * kWorkers)
-    paged_join_kernel<T, D, 1><<<dim3((unsigned)all, (unsigned)rows), kJoinThreads, 0, s>>>(k, 16 * nt);
-  else
-    paged_join_kernel<T, D, 4><<<dim3((unsigned)all, (unsigned)((rows + 3) / 4)), kJoinThreads, 0, s>>>(k, 16 * nt);
-  return hipGetLastError();
+  return launch_join<T, D>({k.record, k.part_ml, k.part_o, k.a.o, k.a.osb, k.a.osh, k.a.oss, k.a.lse, k.group, k.blocks, k.a.batch,
+                            k.a.heads_q, k.a.heads_kv, k.a.tokens, k.rows, k.row_blocks, 16 * nt, k.scale_log2}, s);
 }
 
 }  // namespace
