@@ -117,7 +117,7 @@ def lib():
             raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                                "`python -m paper_2410_13276_amd.build` (no CPU fallback exists)")
         L = C.CDLL(LIB_PATH)
-        for name, (args, res) in (*_SIGS.items(), *_DECODE_SIGS.items()):
+        for name, (args, res) in (*_SIGS.items(), *_DECODE_SIGS.items(), *_CACHE_SIGS.items()):
             fn = getattr(L, name)
             fn.argtypes = args
             fn.restype = res
@@ -600,3 +600,8 @@ def bsattn_varlen(q, k, v, cu_seqlens, mask: VarlenMask, *, causal: bool = True,
 from .decode import SIGS as _DECODE_SIGS  # noqa: E402
 from .decode import (alloc_kv_cache, kv_append, paged_attn, paged_attn_workspace_bytes,  # noqa: E402,F401
                      rope, rope_freqs, rope_grad)
+
+# a small cache: held in 4 bits, and cut to the keys of the largest attention weight
+from .cache import SIGS as _CACHE_SIGS  # noqa: E402
+from .cache import (Q4Pool, alloc_kv_cache_q4, kv_append_q4, kv_evict, kv_read, kv_weights, paged_attn_q4,  # noqa: E402,F401
+                    paged_attn_q4_workspace_bytes)

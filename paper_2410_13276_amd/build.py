@@ -15,7 +15,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libseer.so")
 SOURCES = ["gate_kernels.hip", "attn_kernels.hip", "distill_kernels.hip", "rope_kernels.hip",
-           "paged_attn_kernels.hip", "seer_api.cpp", "decode_api.cpp"]
+           "paged_attn_kernels.hip", "q4_kernels.hip", "q4_attn_kernels.hip", "weights_kernels.hip", "evict_kernels.hip",
+           "seer_api.cpp", "decode_api.cpp", "cache_api.cpp"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # packed-FP32 instructions are disabled: plain float code must not be turned

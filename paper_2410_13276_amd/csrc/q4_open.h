@@ -1,0 +1,28 @@
+// q4_open.h -- codes of 4 bits as operands of a matrix product.
+#pragma once
+
+#include "paged_common.h"
+
+namespace seer {
+
+// 1 + c / 16 for c = 7.5, halfway between the codes
+constexpr float kMid = 1.46875f;
+
+#ifdef __HIPCC__
+// The 8 codes of a dword as bf16 1 + c / 16 in the order 0 4 1 5 2 6 3 7, codes 4 to 7 complemented.
+__device__ __forceinline__ bf16x8 open8(uint32_t w) {
+  u32x4 y;
+  y[0] = (w << 3 & 0x00780078u) ^ 0x3ff83f80u;
+  y[1] = (w >> 1 & 0x00780078u) ^ 0x3ff83f80u;
+  y[2] = (w >> 5 & 0x00780078u) ^ 0x3ff83f80u;
+  y[3] = (w >> 9 & 0x00780078u) ^ 0x3ff83f80u;
+  return __builtin_bit_cast(bf16x8, y);
+}
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float x) {
+  return x + __int_as_float(dpp<CTRL>(0, __float_as_int(x)));
+}
+#endif
+
+}  // namespace seer

@@ -80,6 +80,7 @@ _code = None        # torch type -> seer_dtype
 _device = None      # index of the current device
 _raw_stream = None  # device index -> handle of its current stream
 _fn_rope = _fn_append = _fn_paged = _fn_paged_bytes = None
+_fns = {}           # name -> function, of include/seer_cache.h
 
 
 def _load():
@@ -92,6 +93,7 @@ def _load():
         (lambda dev: torch.cuda.current_stream(dev).cuda_stream)
     _fn_rope, _fn_append = lib.seer_rope, lib.seer_kv_append
     _fn_paged, _fn_paged_bytes = lib.seer_paged_attn, lib.seer_paged_attn_workspace_bytes
+    _fns.update((name, getattr(lib, name)) for name in _seer._CACHE_SIGS)
     _t = torch
 
 
