@@ -95,9 +95,18 @@ seer::QueryArgs query_args(const seer_kv_cache* c, const seer_kv_queries* d, con
           sm_scale > 0.f ? sm_scale : (float)(1.0 / std::sqrt((double)c->head_dim))};
 }
 
+// The attention counts page and slot strides in rows of 16 bytes, and of params, in 32 bits.
+seer_status check_near(const seer_kv_cache* c, const seer_kv_pool& p) {
+  for (int i = 0; i < 3; i += 2)
+    if (p.stride[i] / 16 > UINT32_MAX || p.param_stride[i] / (c->head_dim / c->group) > UINT32_MAX) return SEER_ERR_UNSUPPORTED;
+  return SEER_OK;
+}
+
 seer_status check_attn(const seer_kv_cache* c, const seer_kv_queries* d) {
   seer_status s = check_cache(c, true, false);
   if (s == SEER_OK && c->group == 0) s = SEER_ERR_INVALID_ARG;
+  if (s == SEER_OK) s = check_near(c, c->k);
+  if (s == SEER_OK) s = check_near(c, c->v);
   if (s == SEER_OK) s = check_queries(c, d);
   if (s == SEER_OK) s = check_written(d->o_stride, {d->batch, d->heads_q, d->tokens}, c->head_dim, d->dtype);
   return s;

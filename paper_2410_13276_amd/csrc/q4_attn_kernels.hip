@@ -15,19 +15,23 @@
 // what has to be taken out is u times a sum of terms of both signs, which stays as small as the result.  (All of one
 // sign, the second product's sums would be 5 to 100 times the result and carry their rounding into it.)
 //
-// Columns.  A step belongs to a group, so that a group's products may not run into another's sum.  Where a block has
-// few rows (16 / (D / group) at most), its columns are pairs of row and group: the operand Q^T is 0 but in the
-// column's group, which gives S^T by groups in one accumulator, and P^T in column (g, r) is p step_g, of which the
-// outputs of group g take theirs: no weight is formed twice, and the lanes of a row add up its score by two exchanges.  With
-// more rows the columns are rows alone (or of two groups), and the groups are done one after the other.
+// Rows.  A step belongs to a group, so that a group's products may not run into another's sum.  Where a block has
+// few rows (16 / (D / group) at most), the 16 rows of the products' other operand are pairs of row and group: Q is 0 but in
+// the pair's group, which gives S by groups in one accumulator, the groups of a row in one lane, which adds them up;
+// and P^T in column (r, g) is p step_g, of which the outputs of group g take theirs.  With more rows the pairs are rows alone (or
+// of two groups), and the groups are done one after the other.  Weights go from the lanes of their keys to those of the second
+// product's operand through the LDS, so that no weight is formed twice.
 //
 // A wavefront takes 64 keys at a time.  K's codes come to registers as the operand wants them (16 bytes of one
 // key a lane); V's go through the wavefront's own LDS and come back transposed (ds_read_b64_tr_b4: 16 keys of
-// one channel a lane); so do both params, from a token a lane to the 16 keys of a lane's scores.
+// one channel a lane); so do both params.  Where pages hold whole aligned runs of 16 keys, a run's address is formed by the
+// scalar unit.
 //
-// Precision: fp32 statistics and sums; p step enters the second product in three bf16 parts, which hold fp32 whole, and
-// so does a q that is rotated here or fp32 the first.
+// Precision: fp32 statistics and sums.  fp32: q and p step enter in three bf16 parts, which hold fp32 whole.  bf16: p step, and a
+// q that is rotated here, in two, each rounded to nearest: 2^-18 of it off at most, where the output's own rounding is 2^-9 (three
+// parts: 10% more time).
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 #include "paged_join.h"
@@ -42,8 +46,13 @@ constexpr int kWaves = kThreads / kWave;
 constexpr int kKeys = 64;      // of a tile
 constexpr int kWholeKeys = 512;  // rows with room for so many are not split
 
+struct PoolStrides {  // of codes in 16-byte pieces, of params in rows of them
+  uint32_t page, slot, ppage, pslot;
+};
+
 struct KernelArgs {
   Q4AttnArgs a;
+  PoolStrides kst, vst;
   int rows, row_blocks;      // G tokens, blocks of ROWS rows
   FastDiv group, blocks;     // by G and row_blocks
   int capacity;              // tokens that a table row has room for
@@ -66,35 +75,57 @@ __device__ __forceinline__ int units_of(const KernelArgs& k, int len) {
   return max(1, (len + (1 << k.unit_shift) - 1) >> k.unit_shift);
 }
 
-// x[0 .. 7] as three bf16 parts in the order 0 4 1 5 2 6 3 7.
-__device__ __forceinline__ void split3_order(const float (&x)[8], bf16x8 (&y)[3]) {
-  const float z[8] = {x[0], x[4], x[1], x[5], x[2], x[6], x[3], x[7]};
-  split3(z, y);
-}
-
 typedef __attribute__((ext_vector_type(2))) int i32x2;
 
-// D: elements of a head.  NG: groups of a head.  PACK: of them, those that share the columns.  QP: bf16 parts of q.
-// RUN: pages hold whole aligned runs of 16 keys.
+// Largest and sum of a row of 16 lanes, for all of them.
+__device__ __forceinline__ float row_max(float x) {
+  auto with = [&](int y) { x = fmaxf(x, __int_as_float(y)); };
+  with(dpp<0xb1>(0, __float_as_int(x)));   // quad_perm 1 0 3 2
+  with(dpp<0x4e>(0, __float_as_int(x)));   // quad_perm 2 3 0 1
+  with(dpp<0x141>(0, __float_as_int(x)));  // row_half_mirror
+  with(dpp<0x140>(0, __float_as_int(x)));  // row_mirror
+  return x;
+}
+__device__ __forceinline__ float row_sum(float x) {
+  x = dpp_add<0xb1>(x);
+  x = dpp_add<0x4e>(x);
+  x = dpp_add<0x141>(x);
+  return dpp_add<0x140>(x);
+}
+
+// D: elements of a head.  NG: groups of a head.  PACK: of them, those that share the columns.  QP: bf16 parts of q (1: bf16
+// as it is, 2: rotated, 3: fp32).
+// RUN: pages hold whole aligned runs of 16
+// keys, whose rows lie within 2^30 bytes.
 template <typename T, int D, int NG, int PACK, int QP, bool RUN>
 __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   constexpr int ROWS = 16 / PACK, NPH = NG / PACK;
+  constexpr int RV = 4 / PACK;         // rows whose scores a lane holds
   constexpr int NA = D / 16;           // accumulators: 16 channels each
-  constexpr int QD = D / 32;           // dwords of a key's codes per lane; 16-byte pieces of a V row
-  constexpr int NI = QD;               // loads of V's codes per lane
-  constexpr int TQ = 16 / QD;          // tokens of a run that one of them brings
+  constexpr int QD = D / 32;           // dwords of a key's codes per lane
+  constexpr int SIDE = 2;              // sums of the second product that are formed side by side
   constexpr int OSTR = D + 4;
+  constexpr int PSTR = kKeys + 16 / RV;  // (rows of the weights fall on different banks)
   constexpr bool BF = sizeof(T) == 2;
+  constexpr int PP = BF ? 2 : 3;       // bf16 parts of a weight times its step
+  // fp32: what a tile adds is formed by itself, from -1.46875 times the sum of its factors on, and then added; bf16: the
+  // sums run on over the tiles, the factors' own beside them (its rounding, 2^-9, hides what that leaves)
+  constexpr bool RUNS = BF;
   constexpr int kRowCost = 1;          // a row's beginning and end, in units
   constexpr int PIECES = D / 8;
+  constexpr bool HELD = NPH == 1 && QP * QD <= 8;  // Q stays in registers
+  using Piece = std::conditional_t<QD == 4, u32x4, u32x2>;  // a quarter of a row of codes
   __shared__ union {
     struct {
-      u32x4 q[QP][ROWS][PIECES];       // 8 elements in open8's order, 4 to 7 negated
+      u32x4 q[QP][QD][kWave];          // 8 elements in open8's order, 4 to 7 negated, as the lanes read them
       float2 sum[ROWS][NG];            // of a row's elements in a group: as above, and all / 16
       float2 cs[ROWS][D / 2];
       struct {
-        u32x4 v[NI][kWave];
-        uint32_t kp[4][NG][16], vp[4][NG][16];  // params by run, group, key
+        Piece v[kKeys][4];
+        float ks[kKeys][NG], km[kKeys][NG];                    // steps and middles: key, group
+        float vs[4][NG + 1][16], vm[4][NG + 1][16];            // run, group, key
+        float p[ROWS][PSTR];
+        float alpha[ROWS];
       } w[kWaves];
     };
     float o[kWaves][ROWS][OSTR];
@@ -105,12 +136,12 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   const CacheArgs& ca = a.cache;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int n = lane % 16, j = lane / 16;  // column, run of 16 keys
-  const int gp = n / ROWS, row = n % ROWS;
+  const int n = lane % 16, j = lane / 16;
+  const int gp = n % PACK, row = n / PACK;  // of the operand Q's row n, and of column n of the second product
   const int items = ca.heads_kv * ka.row_blocks;  // rows of a sequence
   const int group = ka.group.d;
   const float c = ka.scale_log2;
-  const bool rope = (QP == 3 || !BF) && a.rope.freq != nullptr;
+  const bool rope = QP != 1 && a.rope.freq != nullptr;
   const double freq = (rope ? a.rope.freq : (const double*)ca.k.data)[rope ? min(lane, a.rope.rot / 2 - 1) : 0];
 
   // ---- this workgroup's share (every wavefront works it out by itself)
@@ -144,83 +175,70 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   int at_w = off - item * (row_units + kRowCost);  // position within the row's weight
 
   // ---- a run of one row's units [u0, u1)
-  int u0, u1, h, key0, k_hi;
+  int u0, u1, h, key0, k_hi, last_page;
   const char *kbase, *vbase;
   const uint32_t *kpbase, *vpbase;
   const int32_t* table;
 
-  // K: lane row n of sub-tile i is key 16 (n / 4) + 4 i + n % 4; V's codes: load i brings token 16 j + i TQ + n / QD;
-  // params: token `lane`.
-  const int kk = n / 4 * 16 + n % 4, vk = 16 * j + n / QD;
-  struct Pages {
-    int k[RUN ? 1 : 4], v[RUN ? 1 : NI], p;
+  // K: lane n of sub-tile i is key 16 i + n, a quarter of its row; V's codes: load i brings a quarter of token 16 i + lane / 4;
+  // params: token `lane`.  Where pages hold whole aligned runs, a lane looks up the run of token `lane` alone.
+  struct At {
+    int page;
+    uint32_t slot;
   };
-  // (A key past the run is looked up at the run's last one and then has no page.)
-  auto page_of = [&](int key) -> int {
-    const int page = table[fast_quot(ca.table.page, max(min(key, k_hi - 1), 0))];
-    return key < k_hi ? page : -1;
+  struct Pages {
+    At k[RUN ? 1 : 4], v[RUN ? 1 : 4], p;
+  };
+  // A key's page, as the table has it, and slot.  (A key past the run is taken to be on its last one's page: no branch.
+  // Nothing is done with what is found until it is used, a tile later, as it would be waited for here.)
+  auto page_of = [&](int key) -> At {
+    const int i = fast_quot(ca.table.page, key);
+    return {table[min(i, last_page)], (uint32_t)(key - i * ca.table.page.d)};
   };
   auto pages = [&](int key0) -> Pages {
     Pages p;
-    if constexpr (RUN) {
-      p.k[0] = page_of(key0 + n / 4 * 16);  // (the run's first key: it exists where any of them does)
-      p.v[0] = page_of(key0 + 16 * j);
-      p.p = p.v[0];
-    } else {
+    if constexpr (!RUN) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) p.k[i] = page_of(key0 + kk + 4 * i);
-#pragma unroll
-      for (int i = 0; i < NI; ++i) p.v[i] = page_of(key0 + vk + i * TQ);
-      p.p = page_of(key0 + lane);
+      for (int i = 0; i < 4; ++i) {
+        p.k[i] = page_of(key0 + 16 * i + n);
+        p.v[i] = page_of(key0 + 16 * i + lane / 4);
+      }
     }
+    p.p = page_of(key0 + (RUN ? 16 * j : lane));
     return p;
   };
-  // Page and slot of a key (the pool's first slot where its page is none).
-  struct At {
-    int page, slot;
+  // Offset of a key's row in units of the strides' (the pool's first page where it has none).
+  auto has_page = [&](int page) { return (uint32_t)page < (uint32_t)ca.table.num_pages; };
+  auto offset = [&](const At& s, uint32_t page, uint32_t slot) {
+    return (uint64_t)(has_page(s.page) ? (uint32_t)s.page : 0u) * page + (uint64_t)s.slot * slot;
   };
-  auto place = [&](int page, int key) -> At {
-    const bool ok = (uint32_t)page < (uint32_t)ca.table.num_pages;
-    const int slot = key - fast_quot(ca.table.page, key) * ca.table.page.d;
-    return {ok ? page : 0, ok ? slot : 0};
+  auto run_of = [&](const Pages& pg, int i) -> At {  // (the lanes of a run hold the same)
+    return {__builtin_amdgcn_readlane(pg.p.page, 16 * i), (uint32_t)__builtin_amdgcn_readlane((int)pg.p.slot, 16 * i)};
   };
 
-  uint32_t kq[4][QD];     // K's codes: 8 QD elements of key 16 (n / 4) + 4 i + n % 4
-  u32x4 vq[NI];           // V's, on their way
+  Piece kq[4], vq[4];
   uint32_t kpq[NG], vpq[NG];
   bool there;             // token `lane` exists
-  auto load_k = [&](const Pages& pg, int key0) {
+  // a lane's place within a run
+  const uint32_t klane = (uint32_t)(n * (int)(RUN ? ca.k.ss : 0)) + sizeof(Piece) * j;
+  const uint32_t vlane = (uint32_t)(lane / 4 * (int)(RUN ? ca.v.ss : 0)) + sizeof(Piece) * (lane % 4);
+  auto load_k = [&](const Pages& pg) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const int key = key0 + kk + 4 * i;
-      At s = place(pg.k[RUN ? 0 : i], RUN ? key0 + kk : key);
-      if (RUN) s.slot += 4 * i;
-      const char* p = kbase + s.page * ca.k.sp + s.slot * ca.k.ss;
-      if constexpr (QD == 4) {
-        const u32x4 z = *(const u32x4*)p;
-#pragma unroll
-        for (int f = 0; f < 4; ++f) kq[i][f] = z[f];
-      } else {
-        const u32x2 z = *(const u32x2*)p;
-        kq[i][0] = z[0];
-        kq[i][1] = z[1];
-      }
+      const At s = RUN ? run_of(pg, i) : pg.k[RUN ? 0 : i];
+      kq[i] = *(const Piece*)(kbase + (offset(s, ka.kst.page, ka.kst.slot) << 4) + klane);
     }
   };
   auto load_v = [&](const Pages& pg, int key0) {
 #pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int key = key0 + vk + i * TQ;
-      At s = place(pg.v[RUN ? 0 : i], RUN ? key0 + vk : key);
-      if (RUN) s.slot += i * TQ;
-      // (a piece's place in the LDS goes by the load: the 16 rows that are read together fall on all banks)
-      vq[i] = *(const u32x4*)(vbase + s.page * ca.v.sp + s.slot * ca.v.ss + 16 * ((n ^ i) % QD));
+    for (int i = 0; i < 4; ++i) {
+      const At s = RUN ? run_of(pg, i) : pg.v[RUN ? 0 : i];
+      vq[i] = *(const Piece*)(vbase + (offset(s, ka.vst.page, ka.vst.slot) << 4) + vlane);
     }
-    const int key = key0 + lane;
-    const At s = place(pg.p, key);
-    there = (uint32_t)pg.p < (uint32_t)ca.table.num_pages && key < k_hi;
-    const uint32_t* kp = kpbase + s.page * ca.k.psp + s.slot * ca.k.pss;
-    const uint32_t* vp = vpbase + s.page * ca.v.psp + s.slot * ca.v.pss;
+    there = has_page(pg.p.page) && key0 + lane < k_hi;
+    const At own = {pg.p.page, pg.p.slot + (RUN ? n : 0)};
+    const uint32_t* kp = kpbase + offset(own, ka.kst.ppage, ka.kst.pslot) * NG;
+    const uint32_t* vp = vpbase + offset(own, ka.vst.ppage, ka.vst.pslot) * NG;
     if constexpr (NG == 4) {
       const u32x4 y = *(const u32x4*)kp, z = *(const u32x4*)vp;
 #pragma unroll
@@ -235,6 +253,14 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 
   constexpr int STEP = kWaves * kKeys;
   Pages pn;  // of the tile after the one that is loaded
+  // a thread's 8 elements of Q^T, and the others of their planes; positions of the column's token and of the block's token
+  // that this wavefront turns first
+  constexpr int QW = BF ? 1 : 2;
+  u32x4 q_own[QW], q_other[QW];
+  int col_pos, row_pos[RV], rope_pos = 0;
+  static_assert(ROWS * PIECES <= kThreads, "one piece a thread");
+  const int q_row = min(tid / PIECES, ROWS - 1), q_d0 = tid % PIECES * 8;
+  const bool turns = rope && q_d0 < a.rope.rot;
   auto begin = [&]() -> bool {
     for (;;) {
       if (x >= x_end) return false;
@@ -248,15 +274,33 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
     h = fast_quot(ka.blocks, item);
     key0 = (u0 << ka.unit_shift) + wave * kKeys;
     k_hi = u1 == row_units ? len : u1 << ka.unit_shift;
-    kbase = (const char*)ca.k.data + h * ca.k.sh + 4 * QD * j;
+    last_page = max(fast_quot(ca.table.page, k_hi - 1), 0);
+    kbase = (const char*)ca.k.data + h * ca.k.sh;
     vbase = (const char*)ca.v.data + h * ca.v.sh;
     kpbase = ca.k.params + h * ca.k.psh;
     vpbase = ca.v.params + h * ca.v.psh;
     table = ca.table.ptr + b * ca.table.stride;
     const Pages pg = pages(key0);
     pn = pages(key0 + STEP);
-    load_k(pg, key0);
+    // (all that the run needs before its first scores is asked for ahead of the tile, which it would wait for otherwise)
+    const int r0 = (item - h * ka.row_blocks) * ROWS;
+    col_pos = a.positions[b * a.pos_stride + fast_quot(ka.group, min(r0 + row, ka.rows - 1))];
+#pragma unroll
+    for (int v = 0; v < RV; ++v)
+      row_pos[v] = a.positions[b * a.pos_stride + fast_quot(ka.group, min(r0 + RV * j + v, ka.rows - 1))];
+    if (rope) rope_pos = a.rope_positions[b * a.pos_stride + min(fast_quot(ka.group, r0) + wave, a.tokens - 1)];
+    {
+      const int r = min(r0 + q_row, ka.rows - 1), tk = fast_quot(ka.group, r), half = a.rope.rot / 2;
+      const T* src = (const T*)a.q.ptr + b * a.q.sb + (h * group + (r - tk * group)) * a.q.sh + tk * a.q.ss;
+      const T* other = src + (turns && !a.rope.interleaved ? (q_d0 < half ? q_d0 + half : q_d0 - half) : q_d0);
+#pragma unroll
+      for (int f = 0; f < QW; ++f) {
+        q_own[f] = *((const u32x4*)(src + q_d0) + f);
+        if (QP != 1) q_other[f] = *((const u32x4*)other + f);
+      }
+    }
     load_v(pg, key0);
+    load_k(pg);
     return true;
   };
   bool busy = begin();
@@ -264,7 +308,6 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 
   while (busy) {
     const int r0 = (item - h * ka.row_blocks) * ROWS;  // the first row of the block
-    const int32_t* pos_b = a.positions + b * a.pos_stride;
 
     // ---- Q^T to LDS, rotated: a lane forms its plane's cosine and sine of a token, for all heads
     const int t_first = fast_quot(ka.group, r0);  // of the block's tokens
@@ -274,30 +317,19 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
       if (lane < a.rope.rot / 2) {
         for (int tk = t_first + wave; tk <= t_last; tk += kWaves) {
           float co, si;
-          turn_cos_sin(rate, rpos_b[tk], co, si);
+          turn_cos_sin(rate, tk == t_first + wave ? rope_pos : rpos_b[tk], co, si);
           sh.cs[tk - t_first][lane] = make_float2(co * a.rope.scale, si * a.rope.scale);
         }
       }
       __syncthreads();
     }
-    static_assert(ROWS * PIECES <= kThreads, "one piece a thread");
     if (tid < ROWS * PIECES) {
-      const int rl = tid / PIECES, d0 = tid % PIECES * 8;
-      const int r = min(r0 + rl, ka.rows - 1), tk = fast_quot(ka.group, r);
-      const T* src = (const T*)a.q.ptr + b * a.q.sb + (h * group + (r - tk * group)) * a.q.sh + tk * a.q.ss;
-      const bool turns = rope && d0 < a.rope.rot;
+      const int rl = q_row, d0 = q_d0;
       float y[8], z[8];
-      u32x4 raw[BF ? 1 : 2];
-#pragma unroll
-      for (int f = 0; f < (BF ? 1 : 2); ++f) raw[f] = *((const u32x4*)(src + d0) + f);
-      unpack8(raw, y);
+      unpack8(q_own, y);
       if (turns) {
-        const int half = a.rope.rot / 2;
-        const T* other = src + (a.rope.interleaved ? d0 : d0 < half ? d0 + half : d0 - half);
-#pragma unroll
-        for (int f = 0; f < (BF ? 1 : 2); ++f) raw[f] = *((const u32x4*)other + f);
-        unpack8(raw, z);
-        rotate8(a.rope, sh.cs[tk - t_first], d0, y, z);
+        unpack8(q_other, z);
+        rotate8(a.rope, sh.cs[fast_quot(ka.group, min(r0 + rl, ka.rows - 1)) - t_first], d0, y, z);
       }
       // sums over the group's pieces, which neighbours hold
       const float lo = (y[0] + y[1]) + (y[2] + y[3]), hi = (y[4] + y[5]) + (y[6] + y[7]);
@@ -309,179 +341,235 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 #pragma unroll
       for (int e = 4; e < 8; ++e) y[e] = -y[e];
       const float s8[8] = {y[0], y[4], y[1], y[5], y[2], y[6], y[3], y[7]};
-      if constexpr (QP == 3) {
-        bf16x8 z3[3];
-        split3(s8, z3);
+      bf16x8 parts[QP];
+      split<QP>(s8, parts);  // (a bf16 q that is not rotated is its own first part)
+      // lane (quad of channels, operand row): 0 in the pairs of other groups, where the pairs hold all groups
 #pragma unroll
-        for (int part = 0; part < 3; ++part) sh.q[part][rl][tid % PIECES] = __builtin_bit_cast(u32x4, z3[part]);
-      } else {
-        u32x4 z1;
+      for (int part = 0; part < QP; ++part)
 #pragma unroll
-        for (int f = 0; f < 4; ++f)
-          z1[f] = __builtin_amdgcn_perm(__float_as_uint(s8[2 * f + 1]), __float_as_uint(s8[2 * f]), 0x07060302u);
-        sh.q[0][rl][tid % PIECES] = z1;
-      }
+        for (int g = 0; g < PACK; ++g) {
+          const bool own = NPH > 1 || d0 / (D / NG) == g;
+          sh.q[part][tid % PIECES % QD][16 * (tid % PIECES / QD) + rl * PACK + g] =
+              own ? __builtin_bit_cast(u32x4, parts[part]) : u32x4{0, 0, 0, 0};
+        }
     }
-    // the last key that the lane's column sees (none beyond the rows)
-    const int my_row = min(r0 + row, ka.rows - 1);
-    const int last = min(pos_b[fast_quot(ka.group, my_row)], ka.capacity - 1);
+    // the last key that the lane's column, and its rows, see; and that all rows do
+    const int last = min(col_pos, ka.capacity - 1);
+    int sees[RV], least = last;
+#pragma unroll
+    for (int v = 0; v < RV; ++v) sees[v] = min(row_pos[v], ka.capacity - 1);
+    least = __builtin_amdgcn_readfirstlane(row_min(least));
     __syncthreads();
 
-    // the operand Q^T, 0 but in the column's group (where the columns hold all of them)
     const int quad_group = j * NG / 4;
-    u32x4 q[QP][QD];
-    float2 qsum[NPH];
+    u32x4 q[HELD ? QP : 1][QD];
+    if constexpr (HELD)
 #pragma unroll
-    for (int part = 0; part < QP; ++part)
+      for (int part = 0; part < QP; ++part)
 #pragma unroll
-      for (int i = 0; i < QD; ++i) {
-        q[part][i] = sh.q[part][row][j * QD + i];
-        if constexpr (NPH == 1)
+        for (int i = 0; i < QD; ++i) q[part][i] = sh.q[part][i][lane];
+    f32x4 from[NPH], all[NPH];  // of the lane's pairs of row and group
 #pragma unroll
-          for (int f = 0; f < 4; ++f) q[part][i][f] = quad_group == gp ? q[part][i][f] : 0u;
+    for (int ph = 0; ph < NPH; ++ph)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const float2 y = sh.sum[RV * j + r / PACK][ph * PACK + r % PACK];
+        from[ph][r] = -kMid * y.x;
+        all[ph][r] = y.y;
       }
-#pragma unroll
-    for (int ph = 0; ph < NPH; ++ph) qsum[ph] = sh.sum[row][ph * PACK + gp];
 
     f32x4 acc[NA];
 #pragma unroll
     for (int i = 0; i < NA; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    float m = -INFINITY, l = 0.f, mids[NPH];
+    float m[RV], l[RV], mids[NPH];
 #pragma unroll
-    for (int ph = 0; ph < NPH; ++ph) mids[ph] = 0.f;
+    for (int v = 0; v < RV; ++v) m[v] = -INFINITY, l[v] = 0.f;
+    f32x4 offs[NPH];  // 1.46875 times the sum of the factors, in every element
+#pragma unroll
+    for (int ph = 0; ph < NPH; ++ph) {
+      mids[ph] = 0.f;
+      offs[ph] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    bf16x8 mid8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) mid8[e] = (__bf16)(RUNS ? kMid : -kMid);
 
     auto& st = sh.w[wave];
     for (; key0 < k_hi; key0 += STEP) {
-      // ---- what has arrived goes through the LDS
+      // ---- what has arrived goes through the LDS (a piece's place goes by its token: the 16 rows that are read together
+      // fall on all banks)
 #pragma unroll
-      for (int i = 0; i < NI; ++i) st.v[i][lane] = vq[i];
+      for (int i = 0; i < 4; ++i) st.v[16 * i + lane / 4][lane % 4 ^ (QD == 4 ? lane / 16 : lane / 32)] = vq[i];
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        st.kp[j][g][n] = there ? kpq[g] : 0u;  // (what stands in slots that no row sees may be anything)
-        st.vp[j][g][n] = there ? vpq[g] : 0u;
+        const uint32_t kp = there ? kpq[g] : 0u, vp = there ? vpq[g] : 0u;  // (what stands in slots that no row sees may be anything)
+        st.ks[lane][g] = __uint_as_float(kp << 16);
+        st.km[lane][g] = __uint_as_float(kp & 0xffff0000u);
+        st.vs[j][g][n] = __uint_as_float(vp << 16);
+        st.vm[j][g][n] = __uint_as_float(vp & 0xffff0000u);
       }
-      const uint32_t exist = (uint32_t)(__ballot(there) >> 16 * j) & 0xffffu;
+      const uint64_t exist = __ballot(there);
+      const bool full = exist == ~0ull && key0 + kKeys - 1 <= least;  // all rows see all keys
       __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      const Pages pg = pn;
+      load_v(pg, key0 + STEP);  // (V's registers take the next tile's codes, which the LDS has now)
+      pn = pages(key0 + 2 * STEP);
+      __builtin_amdgcn_sched_barrier(0);
 
-      // ---- S^T: element e is key key0 + 16 j + e of the lane's column
-      float s[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = 0.f;
+      // ---- S: s[i][v] is key key0 + 16 i + n of row RV j + v
+      float s[4][RV];
 #pragma unroll
       for (int ph = 0; ph < NPH; ++ph) {
-        const uint32_t own = quad_group == ph * PACK + gp ? ~0u : 0u;
-        u32x4 kp[4];
+        uint32_t own = quad_group == ph * PACK + gp ? ~0u : 0u;
+        int at = lane;
+        if constexpr (!HELD) asm volatile("" : "+v"(own), "+v"(at));  // (read and masked here each time: kept for all phases, Q would spill)
+        f32x4 y[4];
 #pragma unroll
-        for (int f = 0; f < 4; ++f) kp[f] = *(const u32x4*)&st.kp[j][ph * PACK + gp][4 * f];
+        for (int i = 0; i < 4; ++i) y[i] = from[ph];
+#pragma unroll
+        for (int f = 0; f < QD; ++f) {
+          bf16x8 k8[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) k8[i] = open8(kq[i][f]);
+#pragma unroll
+          for (int part = QP - 1; part >= 0; --part) {
+            u32x4 qq;
+            if constexpr (HELD) qq = q[part][f];
+            else qq = sh.q[part][f][at];
+            if constexpr (NPH > 1)
+#pragma unroll
+              for (int z = 0; z < 4; ++z) qq[z] &= own;
+            // (four sums side by side: a product waits for the one before it in its sum)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              y[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, qq), k8[i], y[i], 0, 0, 0);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float y0 = -kMid * qsum[ph].x;
-          f32x4 y = {y0, y0, y0, y0};
+          float ks[PACK], km[PACK];
 #pragma unroll
-          for (int part = QP - 1; part >= 0; --part)
-#pragma unroll
-            for (int f = 0; f < QD; ++f) {
-              u32x4 qq = q[part][f];
-              if constexpr (NPH > 1)
-#pragma unroll
-                for (int z = 0; z < 4; ++z) qq[z] &= own;
-              y = __builtin_amdgcn_mfma_f32_16x16x32_bf16(open8(kq[i][f]), __builtin_bit_cast(bf16x8, qq), y, 0, 0, 0);
-            }
+          for (int g = 0; g < PACK; ++g) ks[g] = st.ks[16 * i + n][ph * PACK + g], km[g] = st.km[16 * i + n][ph * PACK + g];
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const uint32_t p = kp[i][r];
-            s[4 * i + r] = fmaf(__uint_as_float(p << 16), y[r], fmaf(__uint_as_float(p & 0xffff0000u), qsum[ph].y, s[4 * i + r]));
+            float& x = s[i][r / PACK];
+            const float z = km[r % PACK] * all[ph][r];
+            x = fmaf(ks[r % PACK], y[i][r], ph == 0 && r % PACK == 0 ? z : x + z);
           }
         }
       }
-      if constexpr (PACK >= 2)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = dpp_add<0x128>(s[e]);  // row_ror 8
-      if constexpr (PACK == 4)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = dpp_add<0x124>(s[e]);  // row_ror 4
-
-      const Pages pg = pn;
-      pn = pages(key0 + 2 * STEP);
-      load_k(pg, key0 + STEP);
-      load_v(pg, key0 + STEP);
+      load_k(pg);  // (K's registers take the next tile's codes as soon as the scores are formed)
+      __builtin_amdgcn_sched_barrier(0);
 
       // ---- running maximum and sum; s becomes P
-      const uint32_t seen = exist & ((1u << min(max(last + 1 - (key0 + 16 * j), 0), 16)) - 1u);
+      if (!full) {
 #pragma unroll
-      for (int e = 0; e < 16; ++e) s[e] = seen >> e & 1 ? s[e] : -INFINITY;
-      float mx = s[0];
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int e = 1; e < 16; ++e) mx = fmaxf(mx, s[e]);
-      mx = column_max(mx);
-      if (__ballot(mx > m) != 0) {
-        const float m_new = fmaxf(m, mx);
-        const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - m_new) * c);
-        m = m_new;
-        l *= alpha;
+          for (int v = 0; v < RV; ++v)
+            s[i][v] = (exist >> (16 * i + n) & 1) && key0 + 16 * i + n <= sees[v] ? s[i][v] : -INFINITY;
+      }
+      float mx[RV];
+      bool more = false;
 #pragma unroll
-        for (int ph = 0; ph < NPH; ++ph) mids[ph] *= alpha;
+      for (int v = 0; v < RV; ++v) {
+        mx[v] = row_max(fmaxf(fmaxf(s[0][v], s[1][v]), fmaxf(s[2][v], s[3][v])));
+        more |= mx[v] > m[v];
+      }
+      if (__ballot(more) != 0) {
+#pragma unroll
+        for (int v = 0; v < RV; ++v) {
+          const float m_new = fmaxf(m[v], mx[v]);
+          const float alpha = m_new == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m[v] - m_new) * c);
+          m[v] = m_new;
+          l[v] *= alpha;
+          if (n == 0) st.alpha[RV * j + v] = alpha;
+        }
+        __builtin_amdgcn_wave_barrier();
+        const float alpha = st.alpha[row];
+#pragma unroll
+        for (int ph = 0; ph < NPH; ++ph) {
+          mids[ph] *= alpha;
+          if constexpr (RUNS) offs[ph] *= alpha;
+        }
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
           for (int f = 0; f < 4; ++f) acc[i][f] *= alpha;
       }
-      // (the difference first: the largest score's weight is 1 exactly, however large it is)
-      const float m0 = m == -INFINITY ? 0.f : m;
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        s[e] = __builtin_amdgcn_exp2f((s[e] - m0) * c);
-        l += s[e];
+      for (int v = 0; v < RV; ++v) {
+        // (the difference first: the largest score's weight is 1 exactly, however large it is)
+        const float m0 = m[v] == -INFINITY ? 0.f : m[v];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float p = __builtin_amdgcn_exp2f((s[i][v] - m0) * c);
+          l[v] += p;
+          st.p[RV * j + v][16 * i + n] = p;
+        }
       }
+      __builtin_amdgcn_wave_barrier();
 
-      // ---- O^T, a phase's groups at a time
-      const bool partly = __ballot(seen != exist) != 0;
+      // ---- O^T, a phase's groups at a time: element e is key key0 + 16 j + e of the lane's column
+      f32x4 pe[4];
+#pragma unroll
+      for (int f = 0; f < 4; ++f) pe[f] = *(const f32x4*)&st.p[row][16 * j + 4 * f];
+      const uint32_t seen = (uint32_t)(exist >> 16 * j) & ((1u << min(max(last + 1 - (key0 + 16 * j), 0), 16)) - 1u);
 #pragma unroll
       for (int ph = 0; ph < NPH; ++ph) {
         float p[16], mid[16];
 #pragma unroll
         for (int f = 0; f < 4; ++f) {
-          const u32x4 vp = *(const u32x4*)&st.vp[j][ph * PACK + gp][4 * f];
+          const f32x4 vs = *(const f32x4*)&st.vs[j][ph * PACK + gp][4 * f], vm = *(const f32x4*)&st.vm[j][ph * PACK + gp][4 * f];
 #pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            p[4 * f + r] = __uint_as_float(vp[r] << 16);
-            mid[4 * f + r] = __uint_as_float(vp[r] & 0xffff0000u);
-          }
+          for (int r = 0; r < 4; ++r) p[4 * f + r] = vs[r], mid[4 * f + r] = vm[r];
         }
-        if (partly) {  // (a value that the column does not see must not reach it even as 0 times what it holds)
+        if (!full) {  // (a value that the column does not see must not reach it even as 0 times what it holds)
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
             p[e] = seen >> e & 1 ? p[e] : 0.f;
             mid[e] = seen >> e & 1 ? mid[e] : 0.f;
           }
         }
-        float sum = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-          mids[ph] = fmaf(s[e], mid[e], mids[ph]);
-          p[e] *= e & 4 ? -s[e] : s[e];
-          sum += p[e];
+          mids[ph] = fmaf(pe[e / 4][e % 4], mid[e], mids[ph]);
+          p[e] = pe[e / 4][e % 4] * (e & 4 ? -p[e] : p[e]);
         }
-        const float z0 = -kMid * column_sum(sum);
-        bf16x8 pt[2][3];
+        bf16x8 pt[2][PP];
 #pragma unroll
-        for (int f = 0; f < 2; ++f) {
-          const float x8[8] = {p[8 * f], p[8 * f + 1], p[8 * f + 2], p[8 * f + 3], p[8 * f + 4], p[8 * f + 5], p[8 * f + 6], p[8 * f + 7]};
-          split3_order(x8, pt[f]);
+        for (int f = 0; f < 2; ++f) {  // (in open8's order)
+          const float x8[8] = {p[8 * f], p[8 * f + 4], p[8 * f + 1], p[8 * f + 5], p[8 * f + 2], p[8 * f + 6], p[8 * f + 3], p[8 * f + 7]};
+          split<PP>(x8, pt[f]);
         }
+        if constexpr (!RUNS) offs[ph] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int i = ph * PACK * (NA / NG); i < (ph + 1) * PACK * (NA / NG); ++i) {
-          // 16 keys of channel 16 i + n: the lane's row of the LDS is key 16 j + n
-          const int li = n / TQ;  // the load that brought it
-          const char* row_at = (const char*)&st.v[li][16 * j + n % TQ * QD + ((i / 2) ^ li) % QD] + i % 2 * 8;
-          const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) i32x2*)row_at);
-          f32x4 z = {z0, z0, z0, z0};
+        for (int part = PP - 1; part >= 0; --part)
 #pragma unroll
-          for (int part = 2; part >= 0; --part)
+          for (int f = 0; f < 2; ++f) offs[ph] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mid8, pt[f][part], offs[ph], 0, 0, 0);
+#pragma unroll
+        for (int i = ph * PACK * (NA / NG); i < (ph + 1) * PACK * (NA / NG); i += SIDE) {
+          bf16x8 v8[SIDE][2];
+          f32x4 z[SIDE];
+#pragma unroll
+          for (int y = 0; y < SIDE; ++y) {
+            // 16 keys of channel 16 (i + y) + n: the lane's row of the LDS is key 16 j + n
+            const int piece = QD == 4 ? (i + y) / 2 ^ n / 4 : (i + y) ^ n / 8;
+            const char* row_at = (const char*)&st.v[16 * j + n][piece] + (QD == 4 ? (i + y) % 2 * 8 : 0);
+            const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) i32x2*)row_at);
+            v8[y][0] = open8((uint32_t)v[0]);
+            v8[y][1] = open8((uint32_t)v[1]);
+            z[y] = RUNS ? acc[i + y] : offs[ph];
+          }
+#pragma unroll
+          for (int part = PP - 1; part >= 0; --part)
 #pragma unroll
             for (int f = 0; f < 2; ++f)
-              z = __builtin_amdgcn_mfma_f32_16x16x32_bf16(open8((uint32_t)v[f]), pt[f][part], z, 0, 0, 0);
-          acc[i] += z;
+#pragma unroll
+              for (int y = 0; y < SIDE; ++y) z[y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v8[y][f], pt[f][part], z[y], 0, 0, 0);
+#pragma unroll
+          for (int y = 0; y < SIDE; ++y) acc[i + y] = RUNS ? z[y] : acc[i + y] + z[y];
         }
       }
       __builtin_amdgcn_wave_barrier();  // the tile's LDS is read
@@ -509,21 +597,25 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 
     // ---- the wavefronts' results together
     const int nrows = min(ROWS, ka.rows - r0);
-    l = column_sum(l);
+#pragma unroll
+    for (int v = 0; v < RV; ++v) l[v] = row_sum(l[v]);
 #pragma unroll
     for (int ph = 0; ph < NPH; ++ph) mids[ph] = column_sum(mids[ph]);
     __syncthreads();  // sh.q and the tiles are read
-    if (gp == 0 && j == 0) {
-      sM[wave][row] = m;
-      sL[wave][row] = l;
-    }
+    if (n == 0)
+#pragma unroll
+      for (int v = 0; v < RV; ++v) {
+        sM[wave][RV * j + v] = m[v];
+        sL[wave][RV * j + v] = l[v];
+      }
     if (row < nrows)
 #pragma unroll
       for (int i = 0; i < NA; ++i) {
         const int g = i / (NA / NG);
         if (g % PACK != gp) continue;
 #pragma unroll
-        for (int f = 0; f < 4; ++f) sh.o[wave][row][16 * i + 4 * j + f] = fmaf(16.f, acc[i][f], mids[g / PACK]);
+        for (int f = 0; f < 4; ++f) sh.o[wave][row][16 * i + 4 * j + f] =
+              fmaf(16.f, RUNS ? acc[i][f] - offs[g / PACK][f] : acc[i][f], mids[g / PACK]);
       }
     __syncthreads();
     const int slot = 2 * w + (first_run ? 0 : 1);
@@ -595,15 +687,18 @@ Plan plan(int batch, int heads_q, int heads_kv, int tokens, int head_dim, int el
 
 template <typename T, int D, int NG, int PACK, int QP>
 hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
-  if (k.a.q.cache.table.page.d % 16 == 0) q4_attn_kernel<T, D, NG, PACK, QP, true><<<grid, kThreads, 0, s>>>(k);
+  const int64_t far = (int64_t)1 << 26;  // (16 rows of a run within 2^30 bytes)
+  const CacheArgs& ca = k.a.q.cache;
+  if (ca.table.page.d % 16 == 0 && ca.k.ss < far && ca.v.ss < far) q4_attn_kernel<T, D, NG, PACK, QP, true><<<grid, kThreads, 0, s>>>(k);
   else q4_attn_kernel<T, D, NG, PACK, QP, false><<<grid, kThreads, 0, s>>>(k);
   return hipGetLastError();
 }
 template <typename T, int D, int NG, int PACK>
 hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
   if constexpr (sizeof(T) == 2)
-    if (!k.a.q.rope.freq) return launch<T, D, NG, PACK, 1>(k, grid, s);
-  return launch<T, D, NG, PACK, 3>(k, grid, s);
+    return k.a.q.rope.freq ? launch<T, D, NG, PACK, 2>(k, grid, s) : launch<T, D, NG, PACK, 1>(k, grid, s);
+  else
+    return launch<T, D, NG, PACK, 3>(k, grid, s);
 }
 template <typename T, int D, int NG>
 hipError_t launch(const KernelArgs& k, const Plan& p, dim3 grid, hipStream_t s) {
@@ -636,6 +731,11 @@ hipError_t launch_q4_attn(const Q4AttnArgs& a, hipStream_t s) {
   const Plan p = plan(q.batch, q.heads_q, q.cache.heads_kv, q.tokens, q.cache.head_dim, q.cache.group);
   KernelArgs k;
   k.a = a;
+  auto strides = [&](const PoolView& v) -> PoolStrides {
+    return {(uint32_t)(v.sp / 16), (uint32_t)(v.ss / 16), (uint32_t)(v.psp / p.groups), (uint32_t)(v.pss / p.groups)};
+  };
+  k.kst = strides(q.cache.k);
+  k.vst = strides(q.cache.v);
   k.group = fast_div(p.group);
   k.blocks = fast_div(p.row_blocks);
   k.rows = p.rows;

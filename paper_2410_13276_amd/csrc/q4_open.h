@@ -19,6 +19,21 @@ __device__ __forceinline__ bf16x8 open8(uint32_t w) {
   return __builtin_bit_cast(bf16x8, y);
 }
 
+// x as the sum of N bf16 parts: three hold fp32 exactly (8 significant bits each time); two, each rounded to nearest, are
+// 2^-18 off at most.
+template <int N>
+__device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&y)[N]) {
+  if constexpr (N == 3) {
+    split3(x, y);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) y[0][e] = (__bf16)x[e];
+    if constexpr (N == 2)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) y[1][e] = (__bf16)(x[e] - (float)y[0][e]);
+  }
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x) {
   return x + __int_as_float(dpp<CTRL>(0, __float_as_int(x)));

@@ -117,11 +117,12 @@ def rows_of(x, table, page, n):
 def score(q, k, ks, scale, turn, dtype, pos):
     """Scaled scores of a row q [D] with keys k [n, D] and a bound on their error.  A score is a sum of D terms (and as many
     for the groups), in fp32, each rounded: (2 D + 16) U of scale sum |q| size(k); its scaling and the argument of the power 4 U
-    (1 + |s|).  turn: (freqs, scale, interleaved): q is rotated first, off by rotate's bound."""
+    (1 + |s|).  turn: (freqs, scale, interleaved): q is rotated first, off by rotate's bound, and enters whole (fp32) or in
+    two rounded bf16 parts, 2^-18 of it off."""
     qq, eq = q.double(), torch.zeros(q.shape, dtype=torch.float64)
     if turn is not None:
         qq, eq = rotate(q, pos, *turn)
-        eq = eq + U * qq.abs()
+        eq = eq + (2.0 ** -18 if dtype == torch.bfloat16 else U) * qq.abs()
     x = scale * (k @ qq)
     d = (2 * q.shape[-1] + 16) * U * scale * (ks @ qq.abs()) + 4 * U * (1 + x.abs()) + scale * (ks @ eq)
     return x, d
@@ -131,7 +132,7 @@ def attend(q, kpool, vpool, table, page, pos, scale, turn=None, rope_pos=None):
     """fp64 attention of q [B, Hq, S, D] (CPU) over pools in 4 bits: o, lse and their bounds.
 
     A weight is off by twice its score's error relative to the maximum's and 4 U of the power; o's sums of n terms by (2 n + 16)
-    U of sum p size(v) / sum p."""
+    U of sum p size(v) / sum p; a weight times its step enters whole (fp32) or in two rounded bf16 parts, 2^-18 of it off."""
     B, Hq, S, D = q.shape
     k, v, ks, vs = values(kpool), values(vpool), size(kpool), size(vpool)
     pages, Hkv = k.shape[:2]
@@ -161,7 +162,8 @@ def attend(q, kpool, vpool, table, page, pos, scale, turn=None, rope_pos=None):
                 o[b, h, s] = p @ vb[seen, g] / L
                 lse[b, h, s] = x.max() + torch.log(L)
                 el[b, h, s] = dd + (m + 8) * U * (1 + abs(float(lse[b, h, s])))
-                eo[b, h, s] = (2 * dd + (2 * m + 24) * U) * (p @ vsb[seen, g] / L)
+                part = 2.0 ** -18 if q.dtype == torch.bfloat16 else 0.0
+                eo[b, h, s] = (2 * dd + (2 * m + 24) * U + part) * (p @ vsb[seen, g] / L)
     return o, lse, eo, el
 
 
