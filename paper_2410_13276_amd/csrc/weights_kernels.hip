@@ -3,14 +3,14 @@
 //   out[t] = decay in[t] + sum over the rows r that see t of exp(scale q_r . k_t - lse_r)
 //
 // The half of attention that needs no running maximum: the rows' log-sum-exps are known, so that a key's sum is
-// its own affair.  A wavefront holds 64 keys (32 of fp32) as the operand of S^T = K Q^T and goes through the
-// rows, 16 columns at a time; a lane adds up the weights of its keys over its columns, and the 16 columns are joined at the
-// end.  So the keys are read once however many rows there are, a key belongs to one wavefront, and there are no
-// atomics.  Few rows (a step of generation) are bound by reading K, many (the last tokens of a prompt) by the
-// exponentials.
+// its own affair.  A wavefront holds 64 keys (32 of fp32) as one operand of S = Q K^T and goes through the rows, 16
+// rows of the other operand at a time; a lane adds up its keys' weights over its rows, and the quads of lanes, which hold different
+// rows of the same keys, are joined at the end.  So the keys are read once however many rows there are, a key belongs to one
+// wavefront, and there are no atomics.
 //
 // Units of keys are dealt out to the workgroups as in attention, and keys in 4 bits enter as there
-// (q4_attn_kernels.hip).
+// (q4_attn_kernels.hip).  A head's rows stay in the LDS for all units of a run, where they fit.  Few rows (a step of
+// generation) are bound by reading K, many (the last tokens of a prompt) by the exponentials.
 #include <algorithm>
 
 #include "cache.h"
@@ -20,14 +20,15 @@ namespace seer {
 
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
-constexpr int kWorkers = 512;  // workgroups at most: two for each CU
+constexpr int kRoom = 72 << 10;  // bytes of LDS for rows: two workgroups of a CU hold the rows of 64 tokens of 4 heads of 128 each
 
 struct KernelArgs {
   WeightArgs a;
   int64_t ksp, ksh, kss;  // K's strides in bytes
   int rows;               // G tokens
+  int blocks, held;       // blocks of rows, and those that the LDS holds at a time
   FastDiv group;
   int capacity;           // keys that are counted at most
   int unit_shift;         // log2 of the keys per unit
@@ -45,38 +46,51 @@ __device__ __forceinline__ int units_of(const KernelArgs& k, int len) {
   return (len + (1 << k.unit_shift) - 1) >> k.unit_shift;
 }
 
-// T: type of q, and of the keys where NG is 0 (else: 4 bits, NG groups of a head, PACK of them sharing the columns).
-// QP: bf16 parts of q.  RUN: pages hold whole aligned runs of the keys of a lane.
+// T: type of q, and of the keys where NG is 0 (else: 4 bits, NG groups of a head, PACK of them sharing the operand's rows).
+// QP: bf16 parts of q (1: bf16 as it is, or fp32 keys; 2: rotated; 3: fp32 over 4 bits).
+template <typename T, int D, int NG, int PACK, int QP>
+struct Shape {
+  static constexpr bool BF = sizeof(T) == 2, Q4 = NG != 0, F32 = !BF && !Q4;
+  static constexpr int SUB = F32 ? 2 : 4;              // sub-tiles of 16 keys
+  static constexpr int KT = 16 * SUB;
+  static constexpr int ROWS = 16 / PACK;               // rows of a block
+  static constexpr int STEPS = F32 ? D / 16 : D / 32;  // 16-byte pieces of Q per lane
+  static constexpr int NGX = Q4 ? NG : 1;
+  static constexpr bool TURNS = QP > 1 || F32;         // q may be rotated here
+  struct Row {                                         // of a row in the LDS
+    float lse;                                         // log2
+    int last;                                          // the last key that it sees
+    float2 sum[NGX];                                   // as in q4_attn_kernel
+  };
+  // of a block: the operand as the lanes read it, rows, cosines and sines of their tokens
+  static constexpr int OPERAND = QP * STEPS * kWave * 16;
+  static constexpr int BYTES = OPERAND + ROWS * (int)sizeof(Row) + (TURNS ? ROWS * (D / 2) * 8 : 0);
+  static constexpr int WAVES = !Q4 || PACK > 1 || NG == 1 ? 4 : 2;  // per SIMD, as the registers allow
+};
+
 template <typename T, int D, int NG, int PACK, int QP, bool RUN>
-__global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
-  constexpr bool BF = sizeof(T) == 2, Q4 = NG != 0, F32 = !BF && !Q4;
-  constexpr int SUB = F32 ? 2 : 4;              // sub-tiles of 16 keys
-  constexpr int PK = 4 * SUB;                   // keys of a lane
-  constexpr int KT = 16 * SUB;
-  constexpr int ROWS = 16 / PACK;               // rows of a column block
-  constexpr int CB = PACK > 1 ? 1 : QP == 3 ? 2 : 4;  // column blocks that are in the LDS together
+__global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void weights_kernel(KernelArgs ka) {
+  using S = Shape<T, D, NG, PACK, QP>;
+  constexpr bool BF = S::BF, Q4 = S::Q4, F32 = S::F32;
+  constexpr int SUB = S::SUB, KT = S::KT, ROWS = S::ROWS, STEPS = S::STEPS, NGX = S::NGX;
+  constexpr int RV = 4 / PACK;                  // rows whose scores a lane holds
   constexpr int NPH = Q4 ? NG / PACK : 1;
-  constexpr int STEPS = F32 ? D / 16 : D / 32;  // 16-byte pieces of Q^T per lane
   constexpr int KW = Q4 ? D / 32 : 4 * STEPS;   // dwords of a key per lane
-  constexpr int NGX = Q4 ? NG : 1;
-  constexpr bool TURNS = QP == 3 || F32;        // q may be rotated here
-  __shared__ u32x4 sq[QP][CB][STEPS][kWave];
-  __shared__ float2 scs[TURNS ? CB * ROWS : 1][D / 2];
-  __shared__ float2 ssum[CB * ROWS][NGX];       // as in q4_attn_kernel
-  __shared__ float slse[CB * ROWS];
-  __shared__ int slast[CB * ROWS];
-  __shared__ __attribute__((aligned(16))) uint32_t skp[kWaves][4][NGX][16];
+  extern __shared__ __attribute__((aligned(16))) char room[];
+  __shared__ __attribute__((aligned(16))) float sks[kWaves][Q4 ? KT : 1][NGX], skm[kWaves][Q4 ? KT : 1][NGX];
+  u32x4(*sq)[QP][STEPS][kWave] = (u32x4(*)[QP][STEPS][kWave])room;
+  typename S::Row* srow = (typename S::Row*)(room + ka.held * S::OPERAND);
+  float2(*scs)[D / 2] = (float2(*)[D / 2])(srow + ka.held * ROWS);
 
   const QueryArgs& a = ka.a.q;
   const CacheArgs& ca = a.cache;
   const int tid = threadIdx.x, lane = tid % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const int n = lane % 16, j = lane / 16;  // column, run of PK keys
-  const int gp = n / ROWS, row = n % ROWS;
+  const int n = lane % 16, j = lane / 16;
   const int items = ca.heads_kv;
   const int group = ka.group.d;
   const float c = ka.scale_log2;
-  const bool rope = TURNS && a.rope.freq != nullptr;
+  const bool rope = S::TURNS && a.rope.freq != nullptr;
   const double freq = (rope ? a.rope.freq : (const double*)ca.k.data)[rope ? min(lane, a.rope.rot / 2 - 1) : 0];
 
   // ---- this workgroup's share (every wavefront works it out by itself)
@@ -91,7 +105,7 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
   const TurnRate rate = turn_rate(freq);
   const uint32_t total = (uint32_t)(__builtin_amdgcn_readlane(upto, kWave - 1) * items);
   const int w = blockIdx.x;
-  if ((uint32_t)w >= total) return;  // (a share each at least, or none)
+  if ((uint32_t)w >= total) return;  // (a unit each at least, or none)
   const Deal deal(total, gridDim.x);
   int x = deal.first(w);
   const int x_end = deal.first(w + 1);
@@ -110,41 +124,42 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
   int h = (int)((uint32_t)off / (uint32_t)row_units);
   int u0 = off - h * row_units;  // the next unit of the head
 
-  // Keys' operand: lane row n of sub-tile i is key PK (n / 4) + 4 i + n % 4 of a tile.
-  const int kk = n / 4 * PK + n % 4;
-  int k_hi;
+  // Keys' operand: lane n of sub-tile i is key 16 i + n of a tile; params: token `lane`.
+  int k_hi, last_page;
   const char* kbase;
   const uint32_t* kpbase;
   const int32_t* table;
   uint32_t kq[SUB][KW];
   uint32_t kpq[NGX];
   bool there;  // key `lane` of the tile is counted and its page exists
-  // Page of a key (-1: none) and slot, for places that are read: the pool's first slots where there is none.
   struct At {
     int page, slot;
-    bool ok;
   };
-  auto place = [&](int key) -> At {
-    const int i = fast_quot(ca.table.page, max(min(key, k_hi - 1), 0));
-    const int page = table[i];
-    const bool ok = key < k_hi && (uint32_t)page < (uint32_t)ca.table.num_pages;
-    return {ok ? page : 0, ok ? key - i * ca.table.page.d : 0, ok};
+  struct Pages {
+    At k[SUB], p;
   };
-  auto load = [&](int key0) {
-    const char* run = nullptr;
-    if constexpr (RUN) {  // (the run's first key: it exists where any of them does)
-      const At s = place(key0 + n / 4 * PK);
-      run = kbase + s.page * ka.ksp + (s.slot + n % 4) * ka.kss;
-    }
+  // A key's page, as the table has it, and slot.  (A key past the run is taken to be on its last one's page.)
+  auto page_of = [&](int key) -> At {
+    const int i = fast_quot(ca.table.page, key);
+    return {table[min(i, last_page)], key - i * ca.table.page.d};
+  };
+  auto has_page = [&](int page) { return (uint32_t)page < (uint32_t)ca.table.num_pages; };
+  auto pages = [&](int key0) -> Pages {
+    Pages p;
+    p.p = page_of(key0 + (RUN ? min(lane, KT - 1) / 16 * 16 : min(lane, KT - 1)));
+    if constexpr (!RUN)
+#pragma unroll
+      for (int i = 0; i < SUB; ++i) p.k[i] = page_of(key0 + 16 * i + n);
+    return p;
+  };
+  const int klane = (RUN ? n * (int)ka.kss : 0) + (Q4 ? 4 * KW : 16) * j;
+  auto load = [&](const Pages& pg, int key0) {
 #pragma unroll
     for (int i = 0; i < SUB; ++i) {
-      const char* p;
-      if constexpr (RUN) {
-        p = run + 4 * i * ka.kss;
-      } else {
-        const At s = place(key0 + kk + 4 * i);
-        p = kbase + s.page * ka.ksp + s.slot * ka.kss;
-      }
+      At s;
+      if constexpr (RUN) s = {__builtin_amdgcn_readlane(pg.p.page, 16 * i), __builtin_amdgcn_readlane(pg.p.slot, 16 * i)};
+      else s = pg.k[i];
+      const char* p = kbase + (has_page(s.page) ? s.page : 0) * ka.ksp + s.slot * ka.kss + (uint32_t)klane;
       if constexpr (KW == 2) {
         const u32x2 z = *(const u32x2*)p;
         kq[i][0] = z[0];
@@ -158,11 +173,9 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
         }
       }
     }
-    const int key = key0 + min(lane, KT - 1);
-    const At s = place(key);
-    there = s.ok && lane < KT;
+    there = has_page(pg.p.page) && key0 + lane < k_hi && lane < KT;
     if constexpr (Q4) {
-      const uint32_t* p = kpbase + s.page * ca.k.psp + s.slot * ca.k.pss;
+      const uint32_t* p = kpbase + (has_page(pg.p.page) ? pg.p.page : 0) * ca.k.psp + (pg.p.slot + (RUN ? n : 0)) * ca.k.pss;
       if constexpr (NG == 4) {
         const u32x4 z = *(const u32x4*)p;
 #pragma unroll
@@ -178,12 +191,11 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
   };
 
   // Rows r0 .. of the run's head to the LDS.
-  const int blocks = (ka.rows + ROWS - 1) / ROWS;  // of columns
   auto stage = [&](int r0) {
     const int32_t* pos_b = a.positions + b * a.pos_stride;
-    const int t_first = fast_quot(ka.group, r0);
+    const int rows = ka.held * ROWS, t_first = fast_quot(ka.group, r0);
     if (rope) {
-      const int t_last = fast_quot(ka.group, min(r0 + CB * ROWS, ka.rows) - 1);
+      const int t_last = fast_quot(ka.group, min(r0 + rows, ka.rows) - 1);
       const int32_t* rpos_b = a.rope_positions + b * a.pos_stride;
       if (lane < a.rope.rot / 2) {
         for (int tk = t_first + wave; tk <= t_last; tk += kWaves) {
@@ -194,15 +206,15 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
       }
       __syncthreads();
     }
-    for (int e = tid; e < CB * ROWS * (D / 8); e += kThreads) {
+    for (int e = tid; e < rows * (D / 8); e += kThreads) {
       const int rl = e / (D / 8), piece = e % (D / 8), d0 = 8 * piece;
       const int r = min(r0 + rl, ka.rows - 1), tk = fast_quot(ka.group, r), hq = h * group + (r - tk * group);
       const T* src = (const T*)a.q.ptr + b * a.q.sb + hq * a.q.sh + tk * a.q.ss;
       if (piece == 0) {
         const float lse = ka.a.lse[((int64_t)b * a.heads_q + hq) * a.tokens + tk];
-        slse[rl] = lse * kLog2e;
+        srow[rl].lse = lse * kLog2e;
         // (a row without keys, and one beyond the rows, sees none)
-        slast[rl] = r0 + rl < ka.rows && lse != -INFINITY ? min(pos_b[tk], ka.capacity - 1) : -1;
+        srow[rl].last = r0 + rl < ka.rows && lse != -INFINITY ? min(pos_b[tk], ka.capacity - 1) : -1;
       }
       const bool turns = rope && d0 < a.rope.rot;
       float y[8], z[8];
@@ -218,133 +230,120 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
         unpack8(raw, z);
         rotate8(a.rope, scs[tk - t_first], d0, y, z);
       }
-      const int cb = rl / ROWS, col = rl % ROWS;
+      const int cb = rl / ROWS, at = rl % ROWS * PACK;
       if constexpr (F32) {
 #pragma unroll
         for (int f = 0; f < 2; ++f)
-          sq[0][cb][d0 / 16][(d0 % 16 / 4 + f) * 16 + col] =
+          sq[cb][0][d0 / 16][(d0 % 16 / 4 + f) * 16 + at] =
               u32x4{__float_as_uint(y[4 * f]), __float_as_uint(y[4 * f + 1]), __float_as_uint(y[4 * f + 2]),
                     __float_as_uint(y[4 * f + 3])};
       } else {
-        float s8[8];
         if constexpr (Q4) {
           const float lo = (y[0] + y[1]) + (y[2] + y[3]), hi = (y[4] + y[5]) + (y[6] + y[7]);
           float sgn = lo - hi, all = lo + hi;
           sgn = dpp_add<0xb1>(sgn), all = dpp_add<0xb1>(all);
           sgn = dpp_add<0x4e>(sgn), all = dpp_add<0x4e>(all);
           if constexpr (D / NGX == 64) sgn = dpp_add<0x141>(sgn), all = dpp_add<0x141>(all);
-          if (d0 % (D / NGX) == 0) ssum[rl][d0 / (D / NGX)] = make_float2(sgn, all * 0.0625f);
+          if (d0 % (D / NGX) == 0) srow[rl].sum[d0 / (D / NGX)] = make_float2(sgn, all * 0.0625f);
+          const float s8[8] = {y[0], -y[4], y[1], -y[5], y[2], -y[6], y[3], -y[7]};
 #pragma unroll
-          for (int f = 0; f < 4; ++f) {
-            s8[2 * f] = y[f];
-            s8[2 * f + 1] = -y[4 + f];
-          }
-        } else {
-#pragma unroll
-          for (int f = 0; f < 8; ++f) s8[f] = y[f];
+          for (int f = 0; f < 8; ++f) y[f] = s8[f];
         }
-        // 4 bits: lane 16 j + col holds elements D / 4 j ..; else, of step i, elements 32 i + 8 j ..
+        bf16x8 parts[QP];
+        split<QP>(y, parts);
+        // 4 bits: lane 16 j + row holds elements D / 4 j ..; else, of step i, elements 32 i + 8 j ..
         const int step = Q4 ? piece % STEPS : piece / 4, lane_j = Q4 ? piece / STEPS : piece % 4;
-        if constexpr (QP == 3) {
-          bf16x8 z3[3];
-          split3(s8, z3);
 #pragma unroll
-          for (int part = 0; part < 3; ++part)
+        for (int part = 0; part < QP; ++part)
 #pragma unroll
-            for (int f = 0; f < PACK; ++f) {  // (0 but in the columns of the piece's group)
-              const bool own = PACK == 1 || piece * 8 / (D / NGX) == f;
-              u32x4 y4 = __builtin_bit_cast(u32x4, z3[part]);
-              if (!own) y4 = u32x4{0, 0, 0, 0};
-              sq[part][cb][step][16 * lane_j + f * ROWS + col] = y4;
-            }
-        } else {
-          u32x4 z1;
-#pragma unroll
-          for (int f = 0; f < 4; ++f)
-            z1[f] = __builtin_amdgcn_perm(__float_as_uint(s8[2 * f + 1]), __float_as_uint(s8[2 * f]), 0x07060302u);
-#pragma unroll
-          for (int f = 0; f < PACK; ++f) {
-            const bool own = PACK == 1 || piece * 8 / (D / NGX) == f;
-            sq[0][cb][step][16 * lane_j + f * ROWS + col] = own ? z1 : u32x4{0, 0, 0, 0};
+          for (int f = 0; f < PACK; ++f) {  // (0 but in the pairs of the piece's group, where the pairs hold all groups)
+            const bool own = !Q4 || NPH > 1 || d0 / (D / NGX) == f;
+            sq[cb][part][step][16 * lane_j + at + f] = own ? __builtin_bit_cast(u32x4, parts[part]) : u32x4{0, 0, 0, 0};
           }
-        }
       }
     }
   };
 
+  const int quad_group = j * NGX / 4;
   while (x < x_end) {
     // ---- a run of one head's units [u0, u1)
     const int u1 = min(row_units, u0 + (x_end - x));
+    const int k_lo = u0 << ka.unit_shift;
     k_hi = min(len, u1 << ka.unit_shift);
-    kbase = (const char*)ca.k.data + h * ka.ksh + (Q4 ? 4 * KW : 16) * j;
+    last_page = fast_quot(ca.table.page, k_hi - 1);
+    kbase = (const char*)ca.k.data + h * ka.ksh;
     kpbase = Q4 ? ca.k.params + h * ca.k.psh : nullptr;
     table = ca.table.ptr + b * ca.table.stride;
-    int key0 = (u0 << ka.unit_shift) + wave * KT;
-    load(key0);
+    int key0 = k_lo + wave * KT;
+    {
+      const Pages pg = pages(key0);
+      load(pg, key0);
+    }
+    Pages pn = pages(key0 + kWaves * KT);
     // (all wavefronts take as many turns: the rows of one are staged by all)
-    for (int base = u0 << ka.unit_shift; base < k_hi; base += kWaves * KT) {
-      const bool has = key0 < k_hi;
-      const uint32_t exist = (uint32_t)(__ballot(there) >> PK * j) & ((1u << PK) - 1u);
+    for (int base = k_lo; base < k_hi; base += kWaves * KT) {
+      const uint64_t exist = __ballot(there);
       if constexpr (Q4) {
 #pragma unroll
-        for (int g = 0; g < NG; ++g) skp[wave][j][g][n] = kpq[g];
+        for (int g = 0; g < NG; ++g) {
+          sks[wave][lane][g] = __uint_as_float(kpq[g] << 16);
+          skm[wave][lane][g] = __uint_as_float(kpq[g] & 0xffff0000u);
+        }
         __builtin_amdgcn_wave_barrier();
       }
-      float sum[PK];
+      float sum[SUB];
 #pragma unroll
-      for (int e = 0; e < PK; ++e) sum[e] = 0.f;
-      for (int cb0 = 0; cb0 < blocks; cb0 += CB) {
-        if (blocks > CB || base == u0 << ka.unit_shift) {
+      for (int i = 0; i < SUB; ++i) sum[i] = 0.f;
+      for (int cb0 = 0; cb0 < ka.blocks; cb0 += ka.held) {
+        if (ka.blocks > ka.held || base == k_lo) {
           __syncthreads();
           stage(cb0 * ROWS);
           __syncthreads();
         }
-        for (int cb = cb0; cb < min(cb0 + CB, blocks); ++cb) {
-          const int col = (cb - cb0) * ROWS + row;
-          // S^T: element e is key key0 + PK j + e of the lane's column
-          float s[PK];
+        for (int cb = cb0; cb < min(cb0 + ka.held, ka.blocks); ++cb) {
+          const typename S::Row* rows = srow + (cb - cb0) * ROWS + RV * j;  // the lane's
+          // S: s[i][v] is key key0 + 16 i + n of row RV j + v
+          float s[SUB][RV];
           if constexpr (Q4) {
 #pragma unroll
-            for (int e = 0; e < PK; ++e) s[e] = 0.f;
-            const int quad_group = j * NG / 4;
-#pragma unroll
             for (int ph = 0; ph < NPH; ++ph) {
-              const uint32_t own = quad_group == ph ? ~0u : 0u;
-              const float2 qsum = ssum[col][ph * PACK + gp];
-              u32x4 kp[4];
+              uint32_t own = quad_group == ph ? ~0u : 0u;
+              int at = lane;
+              if constexpr (NPH > 1) asm volatile("" : "+v"(own), "+v"(at));  // (Q is read and masked here each time: kept, it would spill)
+              f32x4 y[SUB], all;
 #pragma unroll
-              for (int f = 0; f < 4; ++f) kp[f] = *(const u32x4*)&skp[wave][j][ph * PACK + gp][4 * f];
-              const float y0 = -kMid * qsum.x;
-              f32x4 y[SUB];
+              for (int r = 0; r < 4; ++r) {
+                const float2 q2 = rows[r / PACK].sum[ph * PACK + r % PACK];
+                all[r] = q2.y;
 #pragma unroll
-              for (int i = 0; i < SUB; ++i) y[i] = f32x4{y0, y0, y0, y0};
+                for (int i = 0; i < SUB; ++i) y[i][r] = -kMid * q2.x;
+              }
 #pragma unroll
-              for (int part = QP - 1; part >= 0; --part)
+              for (int f = 0; f < STEPS; ++f) {
+                bf16x8 k8[SUB];
 #pragma unroll
-                for (int f = 0; f < STEPS; ++f) {
-                  u32x4 q = sq[part][cb - cb0][f][lane];
+                for (int i = 0; i < SUB; ++i) k8[i] = open8(kq[i][f]);
+#pragma unroll
+                for (int part = QP - 1; part >= 0; --part) {
+                  u32x4 q = sq[cb - cb0][part][f][at];
                   if constexpr (NPH > 1)
 #pragma unroll
                     for (int z = 0; z < 4; ++z) q[z] &= own;
 #pragma unroll
                   for (int i = 0; i < SUB; ++i)
-                    y[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(open8(kq[i][f]), __builtin_bit_cast(bf16x8, q), y[i], 0, 0, 0);
+                    y[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), k8[i], y[i], 0, 0, 0);
                 }
+              }
 #pragma unroll
               for (int i = 0; i < SUB; ++i)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                  const uint32_t p = kp[i][r];
-                  s[4 * i + r] = fmaf(__uint_as_float(p << 16), y[i][r],
-                                      fmaf(__uint_as_float(p & 0xffff0000u), qsum.y, s[4 * i + r]));
+                  const int g = ph * PACK + r % PACK;
+                  float& to = s[i][r / PACK];
+                  const float z = skm[wave][16 * i + n][g] * all[r];
+                  to = fmaf(sks[wave][16 * i + n][g], y[i][r], ph == 0 && r % PACK == 0 ? z : to + z);
                 }
             }
-            if constexpr (PACK >= 2)
-#pragma unroll
-              for (int e = 0; e < PK; ++e) s[e] = dpp_add<0x128>(s[e]);  // row_ror 8
-            if constexpr (PACK == 4)
-#pragma unroll
-              for (int e = 0; e < PK; ++e) s[e] = dpp_add<0x124>(s[e]);  // row_ror 4
           } else {
             constexpr int SUMS = F32 ? 2 : 1;  // (partial sums of an fp32 score: one chain rounds off twice as far)
             f32x4 y[SUMS][SUB];
@@ -356,54 +355,69 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
             for (int part = QP - 1; part >= 0; --part)
 #pragma unroll
               for (int f = 0; f < STEPS; ++f) {
-                const u32x4 q = sq[part][cb - cb0][f][lane];
+                const u32x4 q = sq[cb - cb0][part][f][lane];
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) {
                   const u32x4 k4 = {kq[i][4 * f], kq[i][4 * f + 1], kq[i][4 * f + 2], kq[i][4 * f + 3]};
                   if constexpr (BF) {
-                    y[0][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k4),
-                                                                      __builtin_bit_cast(bf16x8, q), y[0][i], 0, 0, 0);
+                    y[0][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q),
+                                                                      __builtin_bit_cast(bf16x8, k4), y[0][i], 0, 0, 0);
                   } else {
 #pragma unroll
                     for (int z = 0; z < 4; ++z)
-                      y[z % SUMS][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(k4[z]), __uint_as_float(q[z]),
+                      y[z % SUMS][i] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(q[z]), __uint_as_float(k4[z]),
                                                                             y[z % SUMS][i], 0, 0, 0);
                   }
                 }
               }
-            if constexpr (F32)
 #pragma unroll
-              for (int i = 0; i < SUB; ++i) y[0][i] += y[1][i];
+            for (int i = 0; i < SUB; ++i)
 #pragma unroll
-            for (int e = 0; e < PK; ++e) s[e] = y[0][e / 4][e % 4];
+              for (int v = 0; v < RV; ++v) s[i][v] = F32 ? y[0][i][v] + y[SUMS - 1][i][v] : y[0][i][v];
           }
-          if (cb == blocks - 1) load(key0 + kWaves * KT);  // the tile's keys are done with
-          const float lse = slse[col];
-          const int last = slast[col] + 1 - (key0 + PK * j);
-          const uint32_t seen = exist & ((1u << min(max(last, 0), PK)) - 1u);
+          if (cb == ka.blocks - 1) {  // the tile's keys are done with: the next one's, and the pages after that
+            load(pn, key0 + kWaves * KT);
+            pn = pages(key0 + 2 * kWaves * KT);
+          }
+          int least = 0x7fffffff, last[RV];
 #pragma unroll
-          for (int e = 0; e < PK; ++e) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[e], c, -lse));
-            sum[e] += seen >> e & 1 ? p : 0.f;
+          for (int v = 0; v < RV; ++v) {
+            last[v] = rows[v].last;
+            least = min(least, last[v]);
+          }
+          const bool all_see = exist == (KT == 64 ? ~0ull : (1ull << KT % 64) - 1) && __ballot(least < key0 + KT - 1) == 0;
+          if (all_see) {
+#pragma unroll
+            for (int v = 0; v < RV; ++v) {
+              const float lse = rows[v].lse;
+#pragma unroll
+              for (int i = 0; i < SUB; ++i) sum[i] += __builtin_amdgcn_exp2f(fmaf(s[i][v], c, -lse));
+            }
+          } else {
+#pragma unroll
+            for (int v = 0; v < RV; ++v) {
+              const float lse = rows[v].lse;
+#pragma unroll
+              for (int i = 0; i < SUB; ++i) {
+                const bool sees = (exist >> (16 * i + n) & 1) && key0 + 16 * i + n <= last[v];
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[i][v], c, -lse));
+                sum[i] += sees ? p : 0.f;
+              }
+            }
           }
         }
       }
-      // the columns together; lane n of a run takes its key n
-      float mine_e = 0.f;
+      // the quads' rows together; quad i takes sub-tile i's keys
+      float own = 0.f;
 #pragma unroll
-      for (int e = 0; e < PK; ++e) {
-        float y = sum[e];
-        y = dpp_add<0x128>(y);
-        y = dpp_add<0x124>(y);
-        y = dpp_add<0x122>(y);
-        y = dpp_add<0x121>(y);
-        mine_e = n == e ? y : mine_e;
+      for (int i = 0; i < SUB; ++i) {
+        const float y = column_sum(sum[i]);
+        own = j == i ? y : own;
       }
-      const int key = key0 + PK * j + n;
-      if (has && n < PK && key < k_hi) {
-        const float y = mine_e * (1.f / PACK);  // (the groups' columns hold the same weights)
+      const int key = key0 + lane;
+      if (lane < KT && key < k_hi) {
         const float* in = ka.a.in + b * ka.a.isb + h * ka.a.ish + key;
-        ka.a.out[b * ka.a.osb + h * ka.a.osh + key] = ka.a.decay != 0.f ? fmaf(ka.a.decay, *in, y) : y;
+        ka.a.out[b * ka.a.osb + h * ka.a.osh + key] = ka.a.decay != 0.f ? fmaf(ka.a.decay, *in, own) : own;
       }
       key0 += kWaves * KT;
     }
@@ -421,38 +435,45 @@ __global__ __launch_bounds__(kThreads, 2) void weights_kernel(KernelArgs ka) {
         }
       }
     }
-    __syncthreads();
   }
 }
 
 template <typename T, int D, int NG, int PACK, int QP>
-hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
-  constexpr int PK = sizeof(T) == 4 && NG == 0 ? 8 : 16;
-  if (k.a.q.cache.table.page.d % PK == 0) weights_kernel<T, D, NG, PACK, QP, true><<<grid, kThreads, 0, s>>>(k);
-  else weights_kernel<T, D, NG, PACK, QP, false><<<grid, kThreads, 0, s>>>(k);
+hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
+  using S = Shape<T, D, NG, PACK, QP>;
+  k.blocks = (k.rows + S::ROWS - 1) / S::ROWS;
+  k.held = std::min(k.blocks, std::max(1, kRoom / S::BYTES));
+  // as many workgroups as the GPU holds at once: by registers, and by the LDS
+  const int lds = k.held * S::BYTES + (S::Q4 ? kWaves * S::KT * NG * 8 : 0);
+  const int per_cu = std::max(1, std::min(S::WAVES * 4 / kWaves, (160 << 10) / (lds + 1024)));
+  const dim3 grid((unsigned)std::min((int64_t)256 * per_cu, units));
+  const size_t room = (size_t)k.held * S::BYTES;
+  const int64_t far = (int64_t)1 << 26;  // (the 16 rows of a run within 2^30 bytes)
+  auto kernel = k.a.q.cache.table.page.d % 16 == 0 && k.kss < far ? weights_kernel<T, D, NG, PACK, QP, true>
+                                                                 : weights_kernel<T, D, NG, PACK, QP, false>;
+  if (lds > 64 << 10) {
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
+    if (e != hipSuccess) return e;
+  }
+  kernel<<<grid, kThreads, room, s>>>(k);
   return hipGetLastError();
 }
 template <typename T, int D, int NG, int PACK>
-hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
-  if constexpr (sizeof(T) == 4 && NG == 0) {
-    return launch<T, D, 0, 1, 1>(k, grid, s);
-  } else {
-    if constexpr (sizeof(T) == 2)
-      if (!k.a.q.rope.freq) return launch<T, D, NG, PACK, 1>(k, grid, s);
-    return launch<T, D, NG, PACK, 3>(k, grid, s);
-  }
+hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
+  if constexpr (sizeof(T) == 4) return launch<T, D, NG, PACK, NG == 0 ? 1 : 3>(k, units, s);
+  else return k.a.q.rope.freq ? launch<T, D, NG, PACK, 2>(k, units, s) : launch<T, D, NG, PACK, 1>(k, units, s);
 }
-// (the groups share the columns where the rows leave room for all of them)
+// (the groups share the operand's rows where these leave room for all of them)
 template <typename T, int D, int NG>
-hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
+hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
   if constexpr (NG > 1)
-    if (k.rows <= 16 / NG) return launch<T, D, NG, NG>(k, grid, s);
-  return launch<T, D, NG, 1>(k, grid, s);
+    if (k.rows <= 16 / NG) return launch<T, D, NG, NG>(k, units, s);
+  return launch<T, D, NG, 1>(k, units, s);
 }
 template <typename T, int D>
-hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
+hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
   const int group = k.a.q.cache.group;
-  return group == 0 ? launch<T, D, 0>(k, grid, s) : group == 32 ? launch<T, D, D / 32>(k, grid, s) : launch<T, D, D / 64>(k, grid, s);
+  return group == 0 ? launch<T, D, 0>(k, units, s) : group == 32 ? launch<T, D, D / 32>(k, units, s) : launch<T, D, D / 64>(k, units, s);
 }
 
 }  // namespace
@@ -470,14 +491,13 @@ hipError_t launch_weights(const WeightArgs& a, hipStream_t s) {
   k.group = fast_div(group);
   k.rows = group * q.tokens;
   k.capacity = std::min(q.cache.table.max_pages * q.cache.table.page.d, a.width);
-  k.unit_shift = q4 || q.bf16 ? 8 : 7;
+  k.unit_shift = q4 || q.bf16 ? 9 : 8;  // a tile for each wavefront
   const int64_t rows = (int64_t)q.batch * q.cache.heads_kv;
   auto units = [&]() -> int64_t { return ((int64_t)k.capacity + ((int64_t)1 << k.unit_shift) - 1) >> k.unit_shift; };
   while ((units() + 1) * rows > (1 << 30)) ++k.unit_shift;
   k.scale_log2 = q.scale * kLog2e * (q4 ? 16.f : 1.f);
-  const dim3 grid((unsigned)std::min((int64_t)kWorkers, units() * rows));
-  if (q.bf16) return q.cache.head_dim == 128 ? launch<uint16_t, 128>(k, grid, s) : launch<uint16_t, 64>(k, grid, s);
-  return q.cache.head_dim == 128 ? launch<float, 128>(k, grid, s) : launch<float, 64>(k, grid, s);
+  if (q.bf16) return q.cache.head_dim == 128 ? launch<uint16_t, 128>(k, units() * rows, s) : launch<uint16_t, 64>(k, units() * rows, s);
+  return q.cache.head_dim == 128 ? launch<float, 128>(k, units() * rows, s) : launch<float, 64>(k, units() * rows, s);
 }
 
 }  // namespace seer
