@@ -155,6 +155,9 @@ typedef struct {
   int32_t* kept;                  /* device [batch][heads_kv][keep], contiguous */
 } seer_kv_eviction;
 
+/* Workspace bytes of seer_kv_evict for `batch` sequences of this cache (0: it needs none, or invalid arguments). */
+size_t seer_kv_evict_workspace_bytes(const seer_kv_cache* cache, int32_t batch);
+
 /*
  * Cuts every sequence to `keep` slots of each KV head: the `first` first and `last` last ones, and of the others those
  * with the largest weights, of equal ones the lower slot (-0 and 0 are equal, NaN is larger than any number; slots from `width` on
@@ -165,10 +168,12 @@ typedef struct {
  * are rotated at their positions, and stored and attended at their slots).
  * The new pages are written while the old ones are read: a page of new_table may not be one that a sequence of the call
  * holds, nor stand in it twice, and weights may not overlap new_weights.  A kept slot whose page is none is not moved.  Every other slot is left as it
- * is.
- * SEER_ERR_UNSUPPORTED: as seer_kv_append, more than 2^16 KV heads or 2^22 pairs of sequence and head.
+ * is.  workspace: device memory of seer_kv_evict_workspace_bytes, 256-byte aligned, not shared with a call that may run at
+ * the same time; its contents need no set-up.  NULL where that is 0.
+ * SEER_ERR_UNSUPPORTED: as seer_kv_append, more than 65535 KV heads or 2^22 pairs of sequence and head.
  */
-seer_status seer_kv_evict(const seer_kv_cache* cache, const seer_kv_eviction* desc, void* stream);
+seer_status seer_kv_evict(const seer_kv_cache* cache, const seer_kv_eviction* desc, void* workspace, size_t workspace_bytes,
+                          void* stream);
 
 #ifdef __cplusplus
 }

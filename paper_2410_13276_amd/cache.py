@@ -32,7 +32,8 @@ SIGS = {
     "seer_paged_attn_q4_workspace_bytes": ([_P, _P], C.c_size_t),
     "seer_paged_attn_q4": ([_P, _P, _P, C.c_float] + [_P] * 6 + [C.c_size_t, _P], C.c_int),
     "seer_kv_weights": ([_P, _P, _P, C.c_float] + [_P] * 6, C.c_int),
-    "seer_kv_evict": ([_P, _P, _P], C.c_int),
+    "seer_kv_evict_workspace_bytes": ([_P, C.c_int32], C.c_size_t),
+    "seer_kv_evict": ([_P, _P, _P, C.c_size_t, _P], C.c_int),
 }
 
 # the header's structures, packed in one piece
@@ -409,7 +410,9 @@ def kv_evict(k_cache, v_cache, table, lengths, weights, new_table, keep: int, *,
                           new_table.stride(0), new_table.shape[1], weights.shape[2], new_weights.shape[2], 0,
                           weights.data_ptr(), new_weights.data_ptr(), *weights.stride()[:2], *new_weights.stride()[:2],
                           kept.data_ptr())
-    status = _d._fns["seer_kv_evict"](cache, desc, _d._raw_stream(dev))
+    need = _d._fns["seer_kv_evict_workspace_bytes"](cache, batch)
+    workspace = _d._t.empty(need, dtype=_d._t.uint8, device=lengths.device) if need else None
+    status = _d._fns["seer_kv_evict"](cache, desc, workspace.data_ptr() if need else None, need, _d._raw_stream(dev))
     if status:
         _seer._check(status, "seer_kv_evict")
     return out

@@ -72,6 +72,7 @@ struct EvictArgs {
   int width, new_width;
   int64_t sb, sh, nsb, nsh;
   int32_t* kept;
+  void* workspace;
 };
 
 hipError_t launch_append_q4(const StoreArgs& a, hipStream_t s);
@@ -80,5 +81,6 @@ hipError_t launch_q4_attn(const Q4AttnArgs& a, hipStream_t s);
 size_t q4_attn_workspace(int batch, int heads_q, int heads_kv, int tokens, int head_dim, int group);
 hipError_t launch_weights(const WeightArgs& a, hipStream_t s);
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s);
+size_t evict_workspace(int batch, int heads_kv, int capacity);
 
 }  // namespace seer

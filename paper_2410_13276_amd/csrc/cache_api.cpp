@@ -187,7 +187,13 @@ seer_status seer_kv_weights(const seer_kv_cache* c, const seer_kv_queries* d, co
                                        static_cast<hipStream_t>(stream)));
 }
 
-seer_status seer_kv_evict(const seer_kv_cache* c, const seer_kv_eviction* d, void* stream) {
+size_t seer_kv_evict_workspace_bytes(const seer_kv_cache* c, int32_t batch) {
+  if (check_cache(c, false, false) != SEER_OK || batch <= 0 || (int64_t)batch * c->heads_kv > kMostPairs) return 0;
+  return seer::evict_workspace(batch, c->heads_kv, c->page_size * c->max_pages);
+}
+
+seer_status seer_kv_evict(const seer_kv_cache* c, const seer_kv_eviction* d, void* workspace, size_t workspace_bytes,
+                          void* stream) {
   seer_status s = check_cache(c, true, true);
   if (s != SEER_OK) return s;
   if (!d || d->batch <= 0 || d->keep <= 0 || d->first < 0 || d->last < 0 || d->width <= 0 || d->reserved != 0)
@@ -206,6 +212,9 @@ seer_status seer_kv_evict(const seer_kv_cache* c, const seer_kv_eviction* d, voi
     if (n[i] > 1 && d->new_stride[i] < d->new_width) return SEER_ERR_INVALID_ARG;
   }
   if ((int64_t)d->batch * c->heads_kv > kMostPairs) return SEER_ERR_UNSUPPORTED;
+  const size_t need = seer::evict_workspace(d->batch, c->heads_kv, c->page_size * c->max_pages);
+  if (need && (!workspace || workspace_bytes < need)) return SEER_ERR_WORKSPACE;
+  if (need && !aligned(workspace, 256)) return SEER_ERR_INVALID_ARG;
   seer::EvictArgs a;
   a.cache = cache_args(c);
   a.batch = d->batch;
@@ -225,6 +234,7 @@ seer_status seer_kv_evict(const seer_kv_cache* c, const seer_kv_eviction* d, voi
   a.nsb = d->new_stride[0];
   a.nsh = d->new_stride[1];
   a.kept = d->kept;
+  a.workspace = workspace;
   return from_hip(seer::launch_evict(a, static_cast<hipStream_t>(stream)));
 }
 

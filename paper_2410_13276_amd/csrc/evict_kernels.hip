@@ -1,9 +1,12 @@
 // evict_kernels.hip -- cutting a paged cache to the keys of the largest weight (seer_kv_evict).
 //
-// One workgroup for each sequence and KV head finds the slots that stay: a radix selection of the least weight
-// that does (three passes over histograms of 11, 11 and 10 bits in the LDS), then one over the slots in
-// their order, which counts, and one which writes.  A second launch moves the keys and values, 16 bytes a thread,
-// whatever they are held as: the places it writes are no places that it reads, so that it needs no order.
+// Which slots stay is found by a radix selection of the least weight that does, as an integer of its order: three
+// histograms of 11, 11 and 10 bits in the LDS, then one pass over the slots in their order, which writes those above the
+// weight and the first ones equal to it.  A workgroup does that for a sequence and KV head, its slots in registers where they
+// fit.  Long rows of few heads are cut into parts, a workgroup each: their histograms go to the workspace and a launch
+// a digit adds them up (no atomics between workgroups); what the parts before a part write follows from
+// the histograms too.  A last launch moves the keys and values, 16 bytes a thread, whatever they are held as: the places it
+// writes are no places that it reads, so that it needs no order.
 #include <algorithm>
 
 #include "cache.h"
@@ -16,14 +19,23 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
+constexpr int kPart = 16384;  // slots of a part of a long row at least
+// of a part in the workspace: three histograms; its slots above the weight by the first and second digit; (the first part's:)
+// the weight's upper bits and how many stay of those that have them, after the first and the second digit
+constexpr int kPartInts = 3 * kBins + 64;
 
 // Order of weights as that of integers: NaN above all.
 __device__ __forceinline__ uint32_t weight_key(float w) { return w != w ? 0xffffffffu : ordered_key(w); }
 
-struct SelectArgs2 {
+struct PickArgs {
   EvictArgs a;
   int capacity;  // slots that a table row has room for
+  int parts;     // of a row
+  int* hist;     // [pair][part][kPartInts]
 };
+
+constexpr int shift_of(int digit) { return digit == 0 ? 21 : digit == 1 ? 10 : 0; }
+constexpr int bits_of(int digit) { return digit == 2 ? 10 : 11; }
 
 // Sum over the workgroup of the waves' values before this wave's, and of all.
 __device__ __forceinline__ int2 before(int mine, int* sh, int wave, int lane) {
@@ -38,99 +50,232 @@ __device__ __forceinline__ int2 before(int mine, int* sh, int wave, int lane) {
   __syncthreads();
   return r;
 }
+__device__ __forceinline__ int wave_total(int x) {
+#pragma unroll
+  for (int off = 32; off >= 1; off >>= 1) x += __shfl_xor(x, off);
+  return x;
+}
 
-__global__ __launch_bounds__(kThreads) void evict_select_kernel(SelectArgs2 ka) {
+// The weight that is looked for, as far as it is known: its upper bits, and how many of those that have them stay.
+struct Known {
+  uint32_t prefix;
+  int left;
+};
+// One digit more, from the counts c0 and c1 of bins 2 t and 2 t + 1 from the top of thread t.
+__device__ __forceinline__ Known narrow(const Known& k, int c0, int c1, int bits, int* shw, int* found, int tid, int wave, int lane) {
+  int up = c0 + c1;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int y = __shfl_up(up, d);
+    if (lane >= d) up += y;
+  }
+  const int2 s = before(__shfl(up, kWave - 1), shw, wave, lane);
+  const int above = s.x + up - c0 - c1;  // keys in higher bins than this thread's
+  if (above < k.left && above + c0 + c1 >= k.left) {
+    const bool first = above + c0 >= k.left;
+    found[0] = kBins - (first ? 1 : 2) - 2 * tid;
+    found[1] = k.left - above - (first ? 0 : c0);
+  }
+  __syncthreads();
+  const Known r = {k.prefix << bits | (uint32_t)found[0], found[1]};
+  __syncthreads();
+  return r;
+}
+
+// A row of weights and what of it is chosen from: slots [lo, hi), of which `want` stay.
+struct Row {
+  const float* weights;
+  float* new_weights;
+  int32_t* kept;
+  int n, taken, lo, hi, want;
+};
+__device__ __forceinline__ Row row_of(const PickArgs& ka, int pair) {
   const EvictArgs& a = ka.a;
-  __shared__ int hist[kBins];
-  __shared__ int shw[kWaves];
-  __shared__ int found[2];
-  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
-  const int b = blockIdx.x / (uint32_t)a.cache.heads_kv, h = blockIdx.x - b * a.cache.heads_kv;
-  const float* weights = a.weights + b * a.sb + h * a.sh;
-  float* new_weights = a.new_weights + b * a.nsb + h * a.nsh;
-  int32_t* kept = a.kept + (int64_t)blockIdx.x * a.keep;
-  const int n = min(max(a.lengths[b], 0), ka.capacity);
-  const int taken = min(n, a.keep);
-  auto weight = [&](int i) { return i < a.width ? weights[i] : 0.f; };
-
-  if (h == 0 && tid == 0) a.new_lengths[b] = taken;
-  for (int64_t i = taken + tid; i < a.new_width; i += kThreads) new_weights[i] = 0.f;
-  for (int64_t i = taken + tid; i < a.keep; i += kThreads) kept[i] = -1;
+  const int b = pair / (uint32_t)a.cache.heads_kv, h = pair - b * a.cache.heads_kv;
+  Row r;
+  r.weights = a.weights + b * a.sb + h * a.sh;
+  r.new_weights = a.new_weights + b * a.nsb + h * a.nsh;
+  r.kept = a.kept + (int64_t)pair * a.keep;
+  r.n = min(max(a.lengths[b], 0), ka.capacity);
+  r.taken = min(r.n, a.keep);
+  r.lo = a.first;
+  r.hi = r.n - a.last;
+  r.want = r.n > a.keep ? a.keep - a.first - a.last : 0;
+  return r;
+}
+// What needs no choice: the length, the slots that always stay, and what is behind them.
+__device__ __forceinline__ void write_rest(const PickArgs& ka, const Row& r, int pair, int tid) {
+  const EvictArgs& a = ka.a;
+  const int b = pair / (uint32_t)a.cache.heads_kv;
+  if (pair == b * a.cache.heads_kv && tid == 0) a.new_lengths[b] = r.taken;
+  for (int64_t i = r.taken + tid; i < a.new_width; i += kThreads) r.new_weights[i] = 0.f;
+  for (int64_t i = r.taken + tid; i < a.keep; i += kThreads) r.kept[i] = -1;
   auto keep_slot = [&](int to, int slot) {
-    kept[to] = slot;
-    new_weights[to] = weight(slot);
+    r.kept[to] = slot;
+    r.new_weights[to] = slot < a.width ? r.weights[slot] : 0.f;
   };
-  if (n <= a.keep) {
-    for (int i = tid; i < n; i += kThreads) keep_slot(i, i);
+  if (r.n <= a.keep) {
+    for (int i = tid; i < r.n; i += kThreads) keep_slot(i, i);
     return;
   }
   for (int i = tid; i < a.first; i += kThreads) keep_slot(i, i);
-  for (int i = tid; i < a.last; i += kThreads) keep_slot(a.keep - a.last + i, n - a.last + i);
-  const int lo = a.first, hi = n - a.last, want = a.keep - a.first - a.last;
-  if (want == 0) return;
+  for (int i = tid; i < a.last; i += kThreads) keep_slot(a.keep - a.last + i, r.n - a.last + i);
+}
 
-  // ---- the want-th largest key of [lo, hi): digit by digit from the top
-  uint32_t prefix = 0;
-  int left = want;  // of the keys that begin with `prefix`
-  for (int pass = 0; pass < 3; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
-    __syncthreads();
-#pragma unroll 4
-    for (int i = lo + tid; i < hi; i += kThreads) {
-      const uint32_t key = weight_key(weight(i));
-      if (pass == 0 || key >> (shift + bits) == prefix) atomicAdd(&hist[key >> shift & ((1u << bits) - 1)], 1);
-    }
-    __syncthreads();
-    // thread t: bins 2 t and 2 t + 1 counted from the top
-    const int c0 = hist[kBins - 1 - 2 * tid], c1 = hist[kBins - 2 - 2 * tid];
-    int up = c0 + c1;
+// A workgroup's slots [lo, hi): a run for each wavefront, which takes EL at a time for each lane.
+template <int EL>
+struct Slots {
+  const Row& r;
+  int width, s0, s1, lane;
+  bool held;  // they are in w
+  float w[EL];
+  __device__ __forceinline__ Slots(const Row& row, int width, int lo, int hi, int wave, int lane)
+      : r(row), width(width), lane(lane) {
+    const int seg = ((hi - lo + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
+    s0 = min(lo + wave * seg, hi);
+    s1 = min(s0 + seg, hi);
+    held = s1 - s0 <= EL * kWave;
+    if (held) fetch(s0);
+  }
+  __device__ __forceinline__ void fetch(int i0) {
 #pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const int y = __shfl_up(up, d);
-      if (lane >= d) up += y;
+    for (int f = 0; f < EL; ++f) {
+      const int at = i0 + f * kWave + lane;
+      w[f] = at < s1 && at < width ? r.weights[at] : 0.f;
     }
-    const int2 s = before(__shfl(up, kWave - 1), shw, wave, lane);
-    const int above = s.x + up - c0 - c1;  // keys in higher bins than this thread's
-    if (above < left && above + c0 + c1 >= left) {
-      const bool first = above + c0 >= left;
-      found[0] = kBins - (first ? 1 : 2) - 2 * tid;
-      found[1] = left - above - (first ? 0 : c0);
-    }
-    __syncthreads();
-    prefix = prefix << bits | (uint32_t)found[0];
-    left = found[1];
-    __syncthreads();
   }
+  // use(slot, weight, whether there is one), in the slots' order by wavefronts; the lanes of a wavefront together
+  template <typename Use>
+  __device__ __forceinline__ void each(Use use) {
+    for (int i0 = s0; i0 < s1; i0 += EL * kWave) {
+      if (!held) fetch(i0);
+#pragma unroll
+      for (int f = 0; f < EL; ++f) {
+        if (i0 + f * kWave >= s1) break;
+        const int at = i0 + f * kWave + lane;
+        use(at, w[f], at < s1);
+      }
+    }
+  }
+};
 
-  // ---- in order: a wavefront takes a run of slots, counts those above the key and those equal to it, and then
-  // writes; of the equal ones the first `left` stay
-  const int seg = ((hi - lo + kWaves - 1) / kWaves + kWave - 1) / kWave * kWave;
-  const int s0 = min(lo + wave * seg, hi), s1 = min(s0 + seg, hi);
-  int above = 0, equal = 0;
-#pragma unroll 4
-  for (int i = s0; i < s1; i += kWave) {
-    const int at = i + lane;
-    const uint32_t key = at < s1 ? weight_key(weight(at)) : 0u;
-    above += (int)__popcll(__ballot(at < s1 && key > prefix));
-    equal += (int)__popcll(__ballot(at < s1 && key == prefix));
-  }
-  int above_at = before(above, shw, wave, lane).x, equal_at = before(equal, shw, wave, lane).x;
-#pragma unroll 4
-  for (int i = s0; i < s1; i += kWave) {
-    const int at = i + lane;
-    const float w = at < s1 ? weight(at) : 0.f;
+template <int EL>
+__device__ __forceinline__ void count_digit(Slots<EL>& slots, const Known& k, int digit, int* hist, int tid) {
+  const int shift = shift_of(digit), bits = bits_of(digit);
+  for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+  __syncthreads();
+  slots.each([&](int, float w, bool in) {
     const uint32_t key = weight_key(w);
-    const uint64_t gt = __ballot(at < s1 && key > prefix), eq = __ballot(at < s1 && key == prefix);
-    const int eq_before = equal_at + (int)__popcll(eq & lanemask_lt());
-    const bool stays = (gt >> lane & 1) || ((eq >> lane & 1) && eq_before < left);
-    if (stays) {
-      const int to = a.first + above_at + (int)__popcll(gt & lanemask_lt()) + min(eq_before, left);
-      kept[to] = at;
-      new_weights[to] = w;
+    if (in && (digit == 0 || key >> (shift + bits) == k.prefix)) atomicAdd(&hist[key >> shift & ((1u << bits) - 1)], 1);
+  });
+  __syncthreads();
+}
+
+// The slots that stay to kept and new_weights, from place `above` + the equal ones taken before (`equal` are before).
+template <int EL>
+__device__ __forceinline__ void write_kept(Slots<EL>& slots, const Row& r, const Known& k, int above, int equal, int* shw, int wave,
+                                           int lane) {
+  int gts = 0, eqs = 0;
+  slots.each([&](int, float w, bool in) {
+    const uint32_t key = weight_key(w);
+    gts += (int)__popcll(__ballot(in && key > k.prefix));
+    eqs += (int)__popcll(__ballot(in && key == k.prefix));
+  });
+  above += before(gts, shw, wave, lane).x;
+  equal += before(eqs, shw, wave, lane).x;
+  slots.each([&](int at, float w, bool in) {
+    const uint32_t key = weight_key(w);
+    const uint64_t gt = __ballot(in && key > k.prefix), eq = __ballot(in && key == k.prefix);
+    const int eq_before = equal + (int)__popcll(eq & lanemask_lt());
+    if ((gt >> lane & 1) || ((eq >> lane & 1) && eq_before < k.left)) {
+      const int to = r.lo + above + (int)__popcll(gt & lanemask_lt()) + min(eq_before, k.left);
+      r.kept[to] = at;
+      r.new_weights[to] = w;
     }
-    above_at += (int)__popcll(gt);
-    equal_at += (int)__popcll(eq);
+    above += (int)__popcll(gt);
+    equal += (int)__popcll(eq);
+  });
+}
+
+// A row whole.
+template <int EL>
+__global__ __launch_bounds__(kThreads) void evict_pick_kernel(PickArgs ka) {
+  __shared__ int hist[kBins];
+  __shared__ int shw[kWaves], found[2];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const Row r = row_of(ka, blockIdx.x);
+  Slots<EL> slots(r, ka.a.width, r.lo, r.want ? r.hi : r.lo, wave, lane);
+  write_rest(ka, r, blockIdx.x, tid);
+  if (r.want == 0) return;
+  Known k = {0, r.want};
+#pragma unroll 1
+  for (int digit = 0; digit < 3; ++digit) {
+    count_digit(slots, k, digit, hist, tid);
+    k = narrow(k, hist[kBins - 1 - 2 * tid], hist[kBins - 2 - 2 * tid], bits_of(digit), shw, found, tid, wave, lane);
+  }
+  write_kept(slots, r, k, 0, 0, shw, wave, lane);
+}
+
+// A part of a row: DIGIT's histogram of it, or (3) what of it stays.
+template <int EL, int DIGIT>
+__global__ __launch_bounds__(kThreads) void evict_part_kernel(PickArgs ka) {
+  __shared__ int hist[kBins];
+  __shared__ int shw[kWaves], found[2];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int part = blockIdx.x, pair = blockIdx.y;
+  const Row r = row_of(ka, pair);
+  if (DIGIT == 3 && part == 0) write_rest(ka, r, pair, tid);
+  if (r.want == 0) return;
+  // (parts as long as this row asks for)
+  const int each = max(kPart, (r.hi - r.lo + ka.parts - 1) / ka.parts);
+  const int p0 = r.lo + part * each, p1 = min(p0 + each, r.hi), parts = (r.hi - r.lo + each - 1) / each;
+  if (p0 >= r.hi) return;
+  Slots<EL> slots(r, ka.a.width, p0, p1, wave, lane);
+  int* all = ka.hist + (int64_t)pair * ka.parts * kPartInts;
+  int* mine = all + part * kPartInts;
+  Known k = {0, r.want};
+  if constexpr (DIGIT > 0) {
+    // the digit before, from all parts' histograms of it; what went before that stands behind the first part's
+    constexpr int D0 = DIGIT - 1;
+    const int b0 = kBins - 1 - 2 * tid, b1 = b0 - 1;
+    int c0 = 0, c1 = 0, m0 = 0, m1 = 0;
+    if (D0 > 0) k = {(uint32_t)all[3 * kBins + (D0 == 1 ? 3 : 5)], all[3 * kBins + (D0 == 1 ? 4 : 6)]};
+#pragma unroll 8
+    for (int i = 0; i < parts; ++i) {
+      const int* h = all + i * kPartInts + D0 * kBins;
+      const int x0 = h[b0], x1 = h[b1];
+      if (i < part) m0 += x0, m1 += x1;
+      c0 += x0;
+      c1 += x1;
+    }
+    const int own0 = mine[D0 * kBins + b0], own1 = mine[D0 * kBins + b1];
+    k = narrow(k, c0, c1, bits_of(D0), shw, found, tid, wave, lane);
+    const int bin = (int)(k.prefix & ((1u << bits_of(D0)) - 1));
+    if constexpr (DIGIT < 3) {
+      // for the launches behind: the weight so far, and how many of the part's slots are above it by this digit
+      const int above = before(wave_total((b0 > bin ? own0 : 0) + (b1 > bin ? own1 : 0)), shw, wave, lane).y;
+      if (tid == 0) {
+        mine[3 * kBins + D0] = above;
+        if (part == 0) {
+          // (a place for each digit's: a part of this launch may still read the one before)
+          int* to = all + 3 * kBins + (D0 == 0 ? 3 : 5);
+          to[0] = (int)k.prefix;
+          to[1] = k.left;
+        }
+      }
+    } else {
+      // slots before this part's that are above the weight, and those equal to it
+      int above = (b0 > bin ? m0 : 0) + (b1 > bin ? m1 : 0);
+      if (tid < part) above += all[tid * kPartInts + 3 * kBins] + all[tid * kPartInts + 3 * kBins + 1];
+      if (b0 == bin || b1 == bin) found[0] = b0 == bin ? m0 : m1;
+      above = before(wave_total(above), shw, wave, lane).y;  // (its barriers also publish found)
+      write_kept(slots, r, k, above, found[0], shw, wave, lane);
+      return;
+    }
+  }
+  if constexpr (DIGIT < 3) {
+    count_digit(slots, k, DIGIT, hist, tid);
+    for (int i = tid; i < kBins; i += kThreads) mine[DIGIT * kBins + i] = hist[i];
   }
 }
 
@@ -173,6 +318,11 @@ __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs ka) {
   }
 }
 
+// Parts of a row: as many as give the GPU work, of kPart slots or more.
+int parts_of(int64_t pairs, int capacity) {
+  return (int)std::max((int64_t)1, std::min({((int64_t)capacity + kPart - 1) / kPart, 256 / pairs, (int64_t)32}));
+}
+
 template <int LANES, int PARAMS>
 hipError_t move(const MoveArgs& m, hipStream_t s) {
   const int64_t blocks = (m.entries * LANES + 255) / 256;
@@ -182,10 +332,26 @@ hipError_t move(const MoveArgs& m, hipStream_t s) {
 
 }  // namespace
 
+size_t evict_workspace(int batch, int heads_kv, int capacity) {
+  const int parts = parts_of((int64_t)batch * heads_kv, capacity);
+  return parts > 1 ? (size_t)batch * heads_kv * parts * kPartInts * sizeof(int) : 0;
+}
+
 hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
-  SelectArgs2 k = {a, a.cache.table.max_pages * a.cache.table.page.d};
   const int64_t pairs = (int64_t)a.batch * a.cache.heads_kv;
-  evict_select_kernel<<<(unsigned)pairs, kThreads, 0, s>>>(k);
+  const int capacity = a.cache.table.max_pages * a.cache.table.page.d;
+  const PickArgs k = {a, capacity, parts_of(pairs, capacity), (int*)a.workspace};
+  if (k.parts > 1) {
+    const dim3 grid((unsigned)k.parts, (unsigned)pairs);
+    evict_part_kernel<16, 0><<<grid, kThreads, 0, s>>>(k);
+    evict_part_kernel<16, 1><<<grid, kThreads, 0, s>>>(k);
+    evict_part_kernel<16, 2><<<grid, kThreads, 0, s>>>(k);
+    evict_part_kernel<16, 3><<<grid, kThreads, 0, s>>>(k);
+  } else if (capacity <= 4 * kThreads) {
+    evict_pick_kernel<4><<<(unsigned)pairs, kThreads, 0, s>>>(k);
+  } else {
+    evict_pick_kernel<16><<<(unsigned)pairs, kThreads, 0, s>>>(k);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const int size = a.cache.group ? 1 : a.bf16 ? 2 : 4;

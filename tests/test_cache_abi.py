@@ -105,8 +105,8 @@ def eviction(B=2, keep=10, first=1, last=2, lengths=FAKE, nl=FAKE, nt=FAKE, nts=
     return cache._EVICTION.pack(B, keep, first, last, lengths, nl, nt, nts, nw, width, new_width, reserved, w, neww, *st, *nst, kept)
 
 
-def evict(c, e=eviction()):
-    return seer.lib().seer_kv_evict(c, e, None)
+def evict(c, e=eviction(), ws=None, nbytes=0):
+    return seer.lib().seer_kv_evict(c, e, ws, nbytes, None)
 
 
 @pytest.mark.parametrize("kw,status", CACHE_FAULTS)
@@ -201,6 +201,11 @@ def test_more_of_eviction():
                dict(keep=65, new_width=65), dict(new_width=9), dict(width=0), dict(reserved=1), dict(neww=FAKE), dict(st=(-1, 64)),
                dict(nst=(128, 63)), dict(nst=(0, 64)), dict(nts=-1)):
         assert evict(c, eviction(**kw)) == INVALID, kw
+    long_rows = make_cache(page=64, wide=1024)
+    need = seer.lib().seer_kv_evict_workspace_bytes(long_rows, 2)
+    assert need == 2 * 2 * 4 * (3 * 2048 + 64) * 4 and seer.lib().seer_kv_evict_workspace_bytes(c, 2) == 0  # 4 parts of 16384 slots
+    assert evict(long_rows) == WORKSPACE and evict(long_rows, ws=FAKE, nbytes=need - 1) == WORKSPACE
+    assert evict(long_rows, ws=FAKE + 128, nbytes=need) == INVALID
     big = make_cache(H=65535, rows=100)
     assert evict(big, eviction(B=100, st=(0, 0), nst=(1 << 30, 64))) == UNSUPPORTED
 

@@ -107,6 +107,14 @@ def test_long_rows(n):
     check(gen, "q4", 1, 64, 64, 64, [n], n // 3, 4, 16, weights=w, width=n + 7)
 
 
+@pytest.mark.parametrize("ties", [False, True])
+def test_rows_in_parts(ties):
+    """Rows of several workgroups: the weight that decides has equals in all parts, or every slot has the same."""
+    gen = torch.Generator().manual_seed(11)
+    w = torch.randint(0, 50, (2, 2, 50000), generator=gen).float() if not ties else torch.ones(2, 2, 50000)
+    check(gen, "q4", 2, 64, 64, 64, [50000, 17000], 20011, 3, 40, weights=w, width=50000)
+
+
 def test_weights_narrower_than_the_rows():
     """Slots beyond the weights weigh 0."""
     gen = torch.Generator().manual_seed(4)
