@@ -71,45 +71,52 @@ struct Held {
   uint32_t codes, params;
 };
 
+// a - b as d + e exactly.
+struct Two {
+  float d, e;
+};
+__device__ __forceinline__ Two exact_difference(float a, float b) {
+  const float d = a - b, back = d - a;
+  return {d, (a - (d - back)) - (b + back)};
+}
+
 // 8 elements of a group that LANES neighbours hold.
 template <int LANES>
 __device__ __forceinline__ Held hold(const float (&x)[8]) {
+  // (maximum and minimum are NaN where an element is)
   float hi = x[0], lo = x[0];
-  bool fine = true;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    hi = fmaxf(hi, x[i]);
-    lo = fminf(lo, x[i]);
-    fine &= fabsf(x[i]) <= 0x1p127f;
+  for (int i = 1; i < 8; ++i) {
+    hi = __builtin_elementwise_maximum(hi, x[i]);
+    lo = __builtin_elementwise_minimum(lo, x[i]);
   }
-  hi = neighbours_max<LANES>(fine ? hi : INFINITY);
+  hi = neighbours_max<LANES>(hi <= 0x1p127f && lo >= -0x1p127f ? hi : INFINITY);
   lo = -neighbours_max<LANES>(-lo);
   if (hi == INFINITY) return {0x88888888u, 0x7fc0u};  // step NaN, middle 0
   const float mid = (float)(__bf16)(0.5f * hi + 0.5f * lo);
-  // the step: candidates from one bf16 number below the quotient's fp32 value on
-  const double reach = fmax((double)hi - (double)mid, (double)mid - (double)lo);
-  uint32_t step = __float_as_uint((float)reach * (1.f / 7.5f)) & 0xffff0000u;
-  step = step >= 0x20000u ? step - 0x10000u : 0u;
+  // the step: the first of three numbers, from the fp32 quotient without its low bits on, from which 7.5 steps reach
+  // (7.5 of them are exact, and so is the difference from what they are compared with, which is near)
+  const Two up = exact_difference(hi, mid), down = exact_difference(mid, lo);
+  const bool lower = down.d > up.d || (down.d == up.d && down.e > up.e);
+  const float reach = lower ? down.d : up.d, rest = lower ? down.e : up.e;
+  uint32_t step = __float_as_uint(reach * (1.f / 7.5f)) & 0xffff0000u;
 #pragma unroll
-  for (int i = 0; i < 3; ++i)
-    if (7.5 * (double)__uint_as_float(step) < reach) step += 0x10000u;
-  if (reach > 0 && step < 0x0d800000u) step = 0x0d800000u;  // 2^-100
+  for (int i = 0; i < 2; ++i)
+    if ((7.5f * __uint_as_float(step) - reach) - rest < 0.f) step += 0x10000u;
+  step = reach > 0.f ? max(step, 0x0d800000u) : 0u;  // 2^-100
   const float s = __uint_as_float(step);
-  const float inv = step ? 1.f / s : 0.f;
+  const float inv = step ? __builtin_amdgcn_rcpf(s) : 0.f;
   uint32_t codes = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const float d = x[i] - mid;
-    const float y = d * inv, b = rintf(y);
-    float f = floorf(y);
+    const float y = fmaf(d, inv, 8.f), b = rintf(y);  // (within 0.5 to 15.5, but for rounding)
+    float f = y;
     if (fabsf(y - b) < 1e-5f) {
-      // x - mid = d + e exactly
-      const float back = d - x[i];
-      const float e = (x[i] - (d - back)) - (mid + back);
-      f = (d - b * s) + e >= 0.f ? b : b - 1.f;
+      const Two z = exact_difference(x[i], mid);
+      f = (z.d - (b - 8.f) * s) + z.e >= 0.f ? b : b - 1.f;
     }
-    const int c = min(max((int)f + 8, 0), 15);
-    codes |= (uint32_t)c << 4 * i;
+    codes |= (uint32_t)f << 4 * i;
   }
   return {codes, step >> 16 | (__float_as_uint(mid) & 0xffff0000u)};
 }
