@@ -18,7 +18,6 @@ from __future__ import annotations
 
 import ctypes as C
 import struct
-from dataclasses import dataclass
 
 import paper_2410_13276_amd as _seer
 
@@ -45,21 +44,43 @@ _EVICTION = struct.Struct("=4i3Qq4i2Q4qQ")     # seer_kv_eviction
 _NO_POOL = (0,) * 8
 
 
-@dataclass(frozen=True)
 class Q4Pool:
     """Pages of keys or values in 4 bits: codes uint8 [pages, heads_kv, page_size, head_dim / 2] (element 2 i in the low half
     of byte i) and params bf16 [pages, heads_kv, page_size, head_dim / group, 2] (step, middle): code c stands for middle +
-    step (c - 7.5).  Both may be transposed views ([pages, page_size, heads_kv, ..] in memory)."""
-    codes: object
-    params: object
+    step (c - 7.5).  Both may be transposed views ([pages, page_size, heads_kv, ..] in memory).  Their layout is looked at once,
+    when the pool is made: the tensors may not be resized or transposed in place afterwards."""
+    __slots__ = ("codes", "params", "shape", "group", "_strides", "_dev")
+
+    def __init__(self, codes, params):
+        t = _d._t or _seer._torch()
+        cn, pn, cs, ps = codes.shape, params.shape, codes.stride(), params.stride()
+        dev = codes.get_device()
+        if (len(cn) != 4 or len(pn) != 5 or cn[:3] != pn[:3] or pn[4] != 2 or pn[3] < 1 or cs[3] != 1 or ps[4] != 1
+                or ps[3] != 2 and pn[3] > 1 or (ps[0] | ps[1] | ps[2]) & 1 or params.get_device() != dev
+                or codes.dtype is not t.uint8 or params.dtype is not t.bfloat16):
+            self._refuse(codes, params)
+        self.codes, self.params = codes, params
+        dim = 2 * cn[3]
+        self.shape = (cn[0], cn[1], cn[2], dim)  # [pages, heads_kv, page_size, head_dim]
+        self.group = dim // pn[3]
+        self._strides = (cs[0], cs[1], cs[2], ps[0] // 2, ps[1] // 2, ps[2] // 2)
+        self._dev = dev
+
+    @staticmethod
+    def _refuse(c, p):
+        torch = _seer._torch()
+        if c.device != p.device:
+            raise ValueError("codes and params must be on one GPU")
+        if c.dtype is not torch.uint8 or p.dtype is not torch.bfloat16:
+            raise TypeError("a Q4Pool holds uint8 codes and bfloat16 params")
+        if c.dim() != 4 or p.dim() != 5 or c.shape[:3] != p.shape[:3] or p.shape[4] != 2 or p.shape[3] < 1:
+            raise ValueError("a Q4Pool holds codes [pages, heads_kv, page_size, head_dim / 2] and params [pages, heads_kv, "
+                             "page_size, head_dim / group, 2]")
+        raise ValueError("a Q4Pool holds each head's codes and params contiguously")
 
     @property
     def head_dim(self) -> int:
-        return 2 * self.codes.shape[3]
-
-    @property
-    def group(self) -> int:
-        return self.head_dim // self.params.shape[3]
+        return self.shape[3]
 
 
 def alloc_kv_cache_q4(num_pages: int, page_size: int, heads_kv: int, head_dim: int, group: int = 32, device="cuda"):
@@ -83,38 +104,18 @@ def _refuse(dev, dtype, **named):
             raise ValueError(f"{name} must have unit last stride")
 
 
-def _refuse_pool(name, pool, dev):
-    """Raises for what is wrong with a pool in 4 bits."""
-    c, p = pool.codes, pool.params
-    for t in (c, p):
-        if not t.is_cuda or t.get_device() != dev:
-            raise ValueError(f"{name} must be on the GPU of the other tensors")
-    if c.dtype is not _d._t.uint8 or p.dtype is not _d._t.bfloat16:
-        raise TypeError(f"{name} must hold uint8 codes and bfloat16 params")
-    if c.dim() != 4 or p.dim() != 5 or c.shape[:3] != p.shape[:3] or p.shape[4] != 2 or p.shape[3] < 1:
-        raise ValueError(f"{name} must hold codes [pages, heads_kv, page_size, head_dim / 2] and params [pages, heads_kv, "
-                         "page_size, head_dim / group, 2]")
-    if c.stride(3) != 1 or p.stride(4) != 1 or (p.stride(3) != 2 and p.shape[3] > 1) or any(s % 2 for s in p.stride()[:3]):
-        raise ValueError(f"{name} must hold each head's codes and params contiguously")
-
-
 def _pool(name, pool, dev, dtype):
     """((pages, heads_kv, page_size, head_dim), group, seer_kv_pool's fields) of a Q4Pool or (group 0) a tensor of dtype."""
-    if isinstance(pool, Q4Pool):
-        c, p = pool.codes, pool.params
-        cs, ps = c.stride(), p.stride()
-        if (c.get_device() != dev or p.get_device() != dev or c.dtype is not _d._t.uint8 or p.dtype is not _d._t.bfloat16
-                or len(cs) != 4 or len(ps) != 5 or c.shape[:3] != p.shape[:3] or p.shape[4] != 2 or p.shape[3] < 1
-                or cs[3] != 1 or ps[4] != 1 or ps[3] != 2 and p.shape[3] > 1 or (ps[0] | ps[1] | ps[2]) & 1):
-            _refuse_pool(name, pool, dev)
-        n0, n1, n2, n3 = c.shape
-        return ((n0, n1, n2, 2 * n3), 2 * n3 // p.shape[3],
-                (c.data_ptr(), p.data_ptr(), cs[0], cs[1], cs[2], ps[0] // 2, ps[1] // 2, ps[2] // 2))
-    if pool.get_device() != dev or (dtype is not None and pool.dtype is not dtype) or pool.stride(-1) != 1:
-        _refuse(dev, pool.dtype if dtype is None else dtype, **{name: pool})
-    if pool.dim() != 4:
+    if type(pool) is Q4Pool:
+        if pool._dev != dev:
+            raise ValueError(f"{name} must be on the GPU of the other tensors")
+        return pool.shape, pool.group, (pool.codes.data_ptr(), pool.params.data_ptr(), *pool._strides)
+    st = pool.stride()
+    if len(st) != 4:
         raise ValueError(f"{name} must be [pages, heads_kv, page_size, head_dim] or a Q4Pool")
-    return tuple(pool.shape), 0, (pool.data_ptr(), 0, *pool.stride()[:3], 0, 0, 0)
+    if pool.get_device() != dev or (dtype is not None and pool.dtype is not dtype) or st[3] != 1:
+        _refuse(dev, pool.dtype if dtype is None else dtype, **{name: pool})
+    return tuple(pool.shape), 0, (pool.data_ptr(), 0, *st[:3], 0, 0, 0)
 
 
 def _cache(k_cache, v_cache, table, dev, dtype, dim, heads=None, code=0):
@@ -127,11 +128,12 @@ def _cache(k_cache, v_cache, table, dev, dtype, dim, heads=None, code=0):
             raise ValueError("the caches must be alike")
     if dim is not None and shape[3] != dim or heads is not None and shape[1] != heads:
         raise ValueError("the caches must be [pages, heads_kv, page_size, head_dim], heads and head_dim those of the tokens")
-    _d._check_int("table", table, dev)
-    if table.dim() != 2 or (table.stride(1) != 1 and table.shape[1] > 1):
+    n, ts = table.shape, table.stride()
+    if table.dtype is not _d._t.int32 or table.get_device() != dev:
+        _d._check_int("table", table, dev)
+    if len(n) != 2 or ts[1] != 1 and n[1] > 1:
         raise ValueError("table must be [rows, pages] with unit last stride")
-    packed = _CACHE.pack(shape[1], shape[3], code, group, shape[2], shape[0], table.shape[0], table.shape[1], table.stride(0),
-                         table.data_ptr(), *kf, *vf)
+    packed = _CACHE.pack(shape[1], shape[3], code, group, shape[2], shape[0], n[0], n[1], ts[0], table.data_ptr(), *kf, *vf)
     return packed, group, shape
 
 
@@ -202,14 +204,14 @@ def kv_read(k_cache, v_cache, table, positions, *, rows=None, dtype=None, out=No
     if stream is not None or _d._device() != dev:
         with _d._elsewhere(dev, stream):
             return kv_read(k_cache, v_cache, table, positions, rows=rows, dtype=dtype, out=out)
-    if isinstance(k_cache, Q4Pool):
+    if type(k_cache) is Q4Pool:
         dtype = (out[0].dtype if out is not None else _d._t.bfloat16) if dtype is None else dtype
     else:
         if dtype is not None and dtype is not k_cache.dtype:
             raise TypeError("a cache of values is read as its own dtype")
         dtype = k_cache.dtype
     code = _dtype(dtype)
-    cache, group, (_, heads, _, dim) = _cache(k_cache, v_cache, table, dev, None if isinstance(k_cache, Q4Pool) else dtype, None,
+    cache, group, (_, heads, _, dim) = _cache(k_cache, v_cache, table, dev, None if type(k_cache) is Q4Pool else dtype, None,
                                               code=code)
     n = positions.shape
     if len(n) == 2:
@@ -368,7 +370,7 @@ def kv_evict(k_cache, v_cache, table, lengths, weights, new_table, keep: int, *,
     if stream is not None or _d._device() != dev:
         with _d._elsewhere(dev, stream):
             return kv_evict(k_cache, v_cache, table, lengths, weights, new_table, keep, first=first, last=last, out=out)
-    if isinstance(k_cache, Q4Pool):
+    if type(k_cache) is Q4Pool:
         code, dtype = _seer.BF16, None
     else:
         code, dtype = _dtype(k_cache.dtype), k_cache.dtype

@@ -234,3 +234,16 @@ def test_pools_are_described():
         seer.alloc_kv_cache_q4(4, 16, 2, 128, group=16, device="cpu")
     with pytest.raises(ValueError):
         seer.alloc_kv_cache_q4(4, 16, 2, 96, group=64, device="cpu")
+
+
+def test_pools_are_checked():
+    kc, _ = seer.alloc_kv_cache_q4(4, 16, 2, 128, device="cpu")
+    assert seer.Q4Pool(kc.codes.transpose(1, 2), kc.params.transpose(1, 2)).shape == (4, 16, 2, 128)
+    for codes, params in ((kc.codes.to(torch.int8), kc.params), (kc.codes, kc.params.to(torch.float16))):
+        with pytest.raises(TypeError):
+            seer.Q4Pool(codes, params)
+    for codes, params in ((kc.codes[0], kc.params), (kc.codes, kc.params[..., 0]), (kc.codes, kc.params[:3]),
+                          (kc.codes.transpose(2, 3), kc.params.transpose(2, 3)), (kc.codes, kc.params.transpose(3, 4)),
+                          (kc.codes[..., ::2], kc.params), (kc.codes, kc.params[..., :1, :1])):
+        with pytest.raises(ValueError):
+            seer.Q4Pool(codes, params)
