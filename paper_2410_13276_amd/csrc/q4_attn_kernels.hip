@@ -212,8 +212,10 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   auto offset = [&](const At& s, uint32_t page, uint32_t slot) {
     return (uint64_t)(has_page(s.page) ? (uint32_t)s.page : 0u) * page + (uint64_t)s.slot * slot;
   };
-  auto run_of = [&](const Pages& pg, int i) -> At {  // (the lanes of a run hold the same)
-    return {__builtin_amdgcn_readlane(pg.p.page, 16 * i), (uint32_t)__builtin_amdgcn_readlane((int)pg.p.slot, 16 * i)};
+  // (a lane forms its run's, for all)
+  auto of_run = [&](uint64_t off, int i) {
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(off >> 32), 16 * i) << 32 |
+           (uint32_t)__builtin_amdgcn_readlane((int)off, 16 * i);
   };
 
   Piece kq[4], vq[4];
@@ -223,18 +225,16 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   const uint32_t klane = (uint32_t)(n * (int)(RUN ? ca.k.ss : 0)) + sizeof(Piece) * j;
   const uint32_t vlane = (uint32_t)(lane / 4 * (int)(RUN ? ca.v.ss : 0)) + sizeof(Piece) * (lane % 4);
   auto load_k = [&](const Pages& pg) {
+    const uint64_t mine = RUN ? offset(pg.p, ka.kst.page, ka.kst.slot) << 4 : 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const At s = RUN ? run_of(pg, i) : pg.k[RUN ? 0 : i];
-      kq[i] = *(const Piece*)(kbase + (offset(s, ka.kst.page, ka.kst.slot) << 4) + klane);
-    }
+    for (int i = 0; i < 4; ++i)
+      kq[i] = *(const Piece*)(kbase + (RUN ? of_run(mine, i) : offset(pg.k[RUN ? 0 : i], ka.kst.page, ka.kst.slot) << 4) + klane);
   };
   auto load_v = [&](const Pages& pg, int key0) {
+    const uint64_t mine = RUN ? offset(pg.p, ka.vst.page, ka.vst.slot) << 4 : 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const At s = RUN ? run_of(pg, i) : pg.v[RUN ? 0 : i];
-      vq[i] = *(const Piece*)(vbase + (offset(s, ka.vst.page, ka.vst.slot) << 4) + vlane);
-    }
+    for (int i = 0; i < 4; ++i)
+      vq[i] = *(const Piece*)(vbase + (RUN ? of_run(mine, i) : offset(pg.v[RUN ? 0 : i], ka.vst.page, ka.vst.slot) << 4) + vlane);
     there = has_page(pg.p.page) && key0 + lane < k_hi;
     const At own = {pg.p.page, pg.p.slot + (RUN ? n : 0)};
     const uint32_t* kp = kpbase + offset(own, ka.kst.ppage, ka.kst.pslot) * NG;

@@ -153,13 +153,19 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
     return p;
   };
   const int klane = (RUN ? n * (int)ka.kss : 0) + (Q4 ? 4 * KW : 16) * j;
+  // Byte offset of a key's row (the pool's first page where it has none).
+  auto offset = [&](const At& s) { return (has_page(s.page) ? s.page : 0) * ka.ksp + s.slot * ka.kss; };
   auto load = [&](const Pages& pg, int key0) {
+    // (a lane forms its run's offset, for all: sixteen scalar products a tile were a third of its time)
+    const int64_t mine = RUN ? offset(pg.p) : 0;
 #pragma unroll
     for (int i = 0; i < SUB; ++i) {
-      At s;
-      if constexpr (RUN) s = {__builtin_amdgcn_readlane(pg.p.page, 16 * i), __builtin_amdgcn_readlane(pg.p.slot, 16 * i)};
-      else s = pg.k[i];
-      const char* p = kbase + (has_page(s.page) ? s.page : 0) * ka.ksp + s.slot * ka.kss + (uint32_t)klane;
+      int64_t off;
+      if constexpr (RUN)
+        off = (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), 16 * i) << 32 |
+                        (uint32_t)__builtin_amdgcn_readlane((int)mine, 16 * i));
+      else off = offset(pg.k[i]);
+      const char* p = kbase + off + (uint32_t)klane;
       if constexpr (KW == 2) {
         const u32x2 z = *(const u32x2*)p;
         kq[i][0] = z[0];
