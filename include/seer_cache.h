@@ -19,7 +19,7 @@
  * 4 bits.  Each `group` (32 or 64) successive elements of a key or value of one head share
  * two bf16 numbers, a step and a middle; element x of code c, 0 to 15, stands for
  *   middle + step (c - 7.5).
- * A token's elements x are held so: middle = bf16(max / 2 + min / 2), to nearest; step the
+ * A token's elements x are held so: middle = bf16(max / 2 + min / 2), in fp32 and to nearest; step the
  * least bf16 number from which 7.5 steps reach every element from the middle (0 where the
  * middle is them all, else at least 2^-100); c = floor((x - middle) / step) + 8, within 0 to
  * 15, decided exactly: the code whose value is nearest, the upper of two equally near ones.  So a value is off
@@ -103,8 +103,9 @@ size_t seer_paged_attn_q4_workspace_bytes(const seer_kv_cache* cache, const seer
  * seer_paged_attn over a cache held in 4 bits: o = softmax(sm_scale q K^T) V over the keys at slots t <=
  * positions[b][s] whose page exists; all that is said there of rows without keys, lse, the joining launch, workspace and
  * reproducibility holds.  rope rotates q at rope_positions[b][s] (NULL: positions[b][s]).  sm_scale at most 2^100.
- * K and V enter as the values that they stand for, exactly; q whole (in fp32 or rotated: three bf16 parts), weights
- * fp32 whole; sums and statistics are fp32, o is rounded once.
+ * K and V enter as the values that they stand for, exactly, and q whole (in fp32 or rotated: three bf16 parts); sums and
+ * statistics are fp32.  A weight times the step of a value enters whole where o is fp32, and where it is bf16 in two bf16
+ * parts, at most 2^-18 of it off; o is rounded once.
  * The cache is read once for each 16 query rows (heads_q / heads_kv x tokens).
  * Unseen slots and their params have no effect.  A seen key whose step is NaN makes the rows that see it NaN, a
  * value the elements of its group.

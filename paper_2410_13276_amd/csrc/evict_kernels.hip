@@ -286,11 +286,20 @@ struct MoveArgs {
 };
 
 // LANES threads move an entry, each 16 bytes of its key and of its value; PARAMS: and a dword of their params.
-template <int LANES, int PARAMS>
+// PAST: past the caches, which pays where more is moved than they hold (168 MB of 4 bits 70.7 -> 57.6 us, 17 MB of bf16 7.7 -> 9.1).
+template <int LANES, int PARAMS, bool PAST>
 __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs ka) {
   const EvictArgs& a = ka.a;
   const int piece = threadIdx.x % LANES;
   const uint32_t keep = a.keep, heads = a.cache.heads_kv;
+  auto fetch = [](const char* p) -> u32x4 {
+    if constexpr (PAST) return __builtin_nontemporal_load((const u32x4*)p);
+    else return *(const u32x4*)p;
+  };
+  auto put = [](char* p, const u32x4& x) {
+    if constexpr (PAST) __builtin_nontemporal_store(x, (u32x4*)p);
+    else *(u32x4*)p = x;
+  };
   for (int64_t e = ((int64_t)blockIdx.x * 256 + threadIdx.x) / LANES; e < ka.entries; e += (int64_t)gridDim.x * (256 / LANES)) {
     const int64_t pair = e / keep;
     const int to = (int)(e - pair * keep), b = (int)(pair / heads), h = (int)(pair - (int64_t)b * heads);
@@ -302,15 +311,15 @@ __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs ka) {
     const int from_page = a.cache.table.ptr[b * a.cache.table.stride + fp];
     if ((uint32_t)from_page >= (uint32_t)a.cache.table.num_pages || (uint32_t)to_page >= (uint32_t)a.cache.table.num_pages) continue;
     const int64_t fs = from - fp * a.cache.table.page.d, ts = to - tp * a.to.page.d;
-    const u32x4 k = *(const u32x4*)((const char*)a.cache.k.data + from_page * ka.ksp + h * ka.ksh + fs * ka.kss + 16 * piece);
-    const u32x4 v = *(const u32x4*)((const char*)a.cache.v.data + from_page * ka.vsp + h * ka.vsh + fs * ka.vss + 16 * piece);
+    const u32x4 k = fetch((const char*)a.cache.k.data + from_page * ka.ksp + h * ka.ksh + fs * ka.kss + 16 * piece);
+    const u32x4 v = fetch((const char*)a.cache.v.data + from_page * ka.vsp + h * ka.vsh + fs * ka.vss + 16 * piece);
     uint32_t kp = 0, vp = 0;
     if (piece < PARAMS) {
       kp = a.cache.k.params[from_page * a.cache.k.psp + h * a.cache.k.psh + fs * a.cache.k.pss + piece];
       vp = a.cache.v.params[from_page * a.cache.v.psp + h * a.cache.v.psh + fs * a.cache.v.pss + piece];
     }
-    *(u32x4*)((char*)a.cache.k.data + to_page * ka.ksp + h * ka.ksh + ts * ka.kss + 16 * piece) = k;
-    *(u32x4*)((char*)a.cache.v.data + to_page * ka.vsp + h * ka.vsh + ts * ka.vss + 16 * piece) = v;
+    put((char*)a.cache.k.data + to_page * ka.ksp + h * ka.ksh + ts * ka.kss + 16 * piece, k);
+    put((char*)a.cache.v.data + to_page * ka.vsp + h * ka.vsh + ts * ka.vss + 16 * piece, v);
     if (piece < PARAMS) {
       ((uint32_t*)a.cache.k.params)[to_page * a.cache.k.psp + h * a.cache.k.psh + ts * a.cache.k.pss + piece] = kp;
       ((uint32_t*)a.cache.v.params)[to_page * a.cache.v.psp + h * a.cache.v.psh + ts * a.cache.v.pss + piece] = vp;
@@ -326,7 +335,9 @@ int parts_of(int64_t pairs, int capacity) {
 template <int LANES, int PARAMS>
 hipError_t move(const MoveArgs& m, hipStream_t s) {
   const int64_t blocks = (m.entries * LANES + 255) / 256;
-  evict_move_kernel<LANES, PARAMS><<<(unsigned)std::min(blocks, (int64_t)1 << 22), 256, 0, s>>>(m);
+  const dim3 grid((unsigned)std::min(blocks, (int64_t)1 << 22));
+  if (m.entries * LANES * 32 > (int64_t)64 << 20) evict_move_kernel<LANES, PARAMS, true><<<grid, 256, 0, s>>>(m);
+  else evict_move_kernel<LANES, PARAMS, false><<<grid, 256, 0, s>>>(m);
   return hipGetLastError();
 }
 

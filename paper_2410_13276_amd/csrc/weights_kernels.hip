@@ -47,7 +47,7 @@ __device__ __forceinline__ int units_of(const KernelArgs& k, int len) {
 }
 
 // T: type of q, and of the keys where NG is 0 (else: 4 bits, NG groups of a head, PACK of them sharing the operand's rows).
-// QP: bf16 parts of q (1: bf16 as it is, or fp32 keys; 2: rotated; 3: fp32 over 4 bits).
+// QP: bf16 parts of q (1: bf16 as it is, or fp32 keys; 3, which hold fp32 whole: rotated, or fp32 over 4 bits).
 template <typename T, int D, int NG, int PACK, int QP>
 struct Shape {
   static constexpr bool BF = sizeof(T) == 2, Q4 = NG != 0, F32 = !BF && !Q4;
@@ -167,13 +167,16 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
       else off = offset(pg.k[i]);
       const char* p = kbase + off + (uint32_t)klane;
       if constexpr (KW == 2) {
-        const u32x2 z = *(const u32x2*)p;
+        const u32x2 z = __builtin_nontemporal_load((const u32x2*)p);
         kq[i][0] = z[0];
         kq[i][1] = z[1];
       } else {
 #pragma unroll
         for (int f = 0; f < KW / 4; ++f) {
-          const u32x4 z = *(const u32x4*)(p + 64 * f);
+          // (codes past the caches: 64 mixed sequences 60 -> 51 us; values that way: 64 rows over 32768 tokens 42 -> 44)
+          u32x4 z;
+          if constexpr (Q4) z = __builtin_nontemporal_load((const u32x4*)(p + 64 * f));
+          else z = *(const u32x4*)(p + 64 * f);
 #pragma unroll
           for (int y = 0; y < 4; ++y) kq[i][4 * f + y] = z[y];
         }
@@ -467,7 +470,7 @@ hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
 template <typename T, int D, int NG, int PACK>
 hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
   if constexpr (sizeof(T) == 4) return launch<T, D, NG, PACK, NG == 0 ? 1 : 3>(k, units, s);
-  else return k.a.q.rope.freq ? launch<T, D, NG, PACK, 2>(k, units, s) : launch<T, D, NG, PACK, 1>(k, units, s);
+  else return k.a.q.rope.freq ? launch<T, D, NG, PACK, 3>(k, units, s) : launch<T, D, NG, PACK, 1>(k, units, s);
 }
 // (the groups share the operand's rows where these leave room for all of them)
 template <typename T, int D, int NG>

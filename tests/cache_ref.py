@@ -117,12 +117,11 @@ def rows_of(x, table, page, n):
 def score(q, k, ks, scale, turn, dtype, pos):
     """Scaled scores of a row q [D] with keys k [n, D] and a bound on their error.  A score is a sum of D terms (and as many
     for the groups), in fp32, each rounded: (2 D + 16) U of scale sum |q| size(k); its scaling and the argument of the power 4 U
-    (1 + |s|).  turn: (freqs, scale, interleaved): q is rotated first, off by rotate's bound, and enters whole (fp32) or in
-    two rounded bf16 parts, 2^-18 of it off."""
+    (1 + |s|).  turn: (freqs, scale, interleaved): q is rotated first, off by rotate's bound, and enters whole."""
     qq, eq = q.double(), torch.zeros(q.shape, dtype=torch.float64)
     if turn is not None:
         qq, eq = rotate(q, pos, *turn)
-        eq = eq + (2.0 ** -18 if dtype == torch.bfloat16 else U) * qq.abs()
+        eq = eq + U * qq.abs()
     x = scale * (k @ qq)
     d = (2 * q.shape[-1] + 16) * U * scale * (ks @ qq.abs()) + 4 * U * (1 + x.abs()) + scale * (ks @ eq)
     return x, d
