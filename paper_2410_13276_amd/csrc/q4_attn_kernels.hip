@@ -113,6 +113,12 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   constexpr bool RUNS = BF;
   constexpr int kRowCost = 1;          // a row's beginning and end, in units
   constexpr int PIECES = D / 8;
+  // with more phases than one, K's codes are brought into the order of their channels, so that a step of the product has
+  // the channels of one group only
+  constexpr bool ALIGNED = NPH > 1 && PACK == 1;
+  // of four phases the sums of Q's groups are read from the LDS each time (28 rows over 8 x 4096 tokens, groups of 32:
+  // held, 55.1 us, with 96 spills; read, 39.3)
+  constexpr bool SUMS_HELD = NPH < 4;
   constexpr bool HELD = NPH == 1 && QP * QD <= 8;  // Q stays in registers
   using Piece = std::conditional_t<QD == 4, u32x4, u32x2>;  // a quarter of a row of codes
   __shared__ union {
@@ -351,7 +357,8 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 #pragma unroll
         for (int g = 0; g < PACK; ++g) {
           const bool own = NPH > 1 || d0 / (D / NG) == g;
-          sh.q[part][tid % PIECES % QD][16 * (tid % PIECES / QD) + rl * PACK + g] =
+          (ALIGNED ? sh.q[part][tid % PIECES / 4][16 * (tid % PIECES % 4) + rl]
+                   : sh.q[part][tid % PIECES % QD][16 * (tid % PIECES / QD) + rl * PACK + g]) =
               own ? __builtin_bit_cast(u32x4, parts[part]) : u32x4{0, 0, 0, 0};
         }
     }
@@ -370,7 +377,8 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
       for (int part = 0; part < QP; ++part)
 #pragma unroll
         for (int i = 0; i < QD; ++i) q[part][i] = sh.q[part][i][lane];
-    f32x4 from[NPH], all[NPH];  // of the lane's pairs of row and group
+    f32x4 from[SUMS_HELD ? NPH : 1], all[SUMS_HELD ? NPH : 1];  // of the lane's pairs of row and group
+    if constexpr (SUMS_HELD)
 #pragma unroll
     for (int ph = 0; ph < NPH; ++ph)
 #pragma unroll
@@ -421,25 +429,45 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 
       // ---- S: s[i][v] is key key0 + 16 i + n of row RV j + v
       float s[4][RV];
+      uint32_t kc[4][QD];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int f = 0; f < QD; ++f) kc[i][f] = kq[i][f];
+        if constexpr (ALIGNED) by_channels(kc[i]);
+      }
 #pragma unroll
       for (int ph = 0; ph < NPH; ++ph) {
         uint32_t own = quad_group == ph * PACK + gp ? ~0u : 0u;
         int at = lane;
         if constexpr (!HELD) asm volatile("" : "+v"(own), "+v"(at));  // (read and masked here each time: kept for all phases, Q would spill)
-        f32x4 y[4];
+        f32x4 y[4], all_ph;
+        if constexpr (SUMS_HELD) {
+          all_ph = all[ph];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) y[i] = from[ph];
+          for (int i = 0; i < 4; ++i) y[i] = from[ph];
+        } else {
+          int at_row = RV * j;
+          asm volatile("" : "+v"(at_row));  // (read here each time)
 #pragma unroll
-        for (int f = 0; f < QD; ++f) {
+          for (int r = 0; r < 4; ++r) {
+            const float2 q2 = sh.sum[at_row + r / PACK][ph * PACK + r % PACK];
+            all_ph[r] = q2.y;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) y[i][r] = -kMid * q2.x;
+          }
+        }
+#pragma unroll
+        for (int f = ALIGNED ? ph * (QD / NG) : 0; f < (ALIGNED ? (ph + 1) * (QD / NG) : QD); ++f) {
           bf16x8 k8[4];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) k8[i] = open8(kq[i][f]);
+          for (int i = 0; i < 4; ++i) k8[i] = open8(kc[i][f]);
 #pragma unroll
           for (int part = QP - 1; part >= 0; --part) {
             u32x4 qq;
             if constexpr (HELD) qq = q[part][f];
             else qq = sh.q[part][f][at];
-            if constexpr (NPH > 1)
+            if constexpr (NPH > 1 && !ALIGNED)
 #pragma unroll
               for (int z = 0; z < 4; ++z) qq[z] &= own;
             // (four sums side by side: a product waits for the one before it in its sum)
@@ -456,7 +484,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             float& x = s[i][r / PACK];
-            const float z = km[r % PACK] * all[ph][r];
+            const float z = km[r % PACK] * all_ph[r];
             x = fmaf(ks[r % PACK], y[i][r], ph == 0 && r % PACK == 0 ? z : x + z);
           }
         }

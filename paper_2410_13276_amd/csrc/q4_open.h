@@ -34,6 +34,29 @@ __device__ __forceinline__ void split(const float (&x)[8], bf16x8 (&y)[N]) {
   }
 }
 
+// A quarter of a key's codes of each of the four rows of 16 lanes (row j: quarter j) as operands whose 32 channels are
+// successive: dword 4 f + j of the key to row j of operand f, by exchanges of rows between two registers.
+template <int N>
+__device__ __forceinline__ void by_channels(uint32_t (&x)[N]) {
+  static_assert(N == 2 || N == 4, "dwords of a quarter");
+  auto swap16 = [](uint32_t& a, uint32_t& b) {  // odd rows of a, even ones of b
+    const auto y = __builtin_amdgcn_permlane16_swap(a, b, false, false);
+    a = y[0], b = y[1];
+  };
+  auto swap32 = [](uint32_t& a, uint32_t& b) {  // the upper half of a, the lower one of b
+    const auto y = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+    a = y[0], b = y[1];
+  };
+  swap16(x[0], x[1]);
+  if constexpr (N == 4) {
+    swap16(x[2], x[3]);
+    swap32(x[0], x[2]);
+    swap32(x[1], x[3]);
+  } else {
+    swap32(x[0], x[1]);
+  }
+}
+
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float x) {
   return x + __int_as_float(dpp<CTRL>(0, __float_as_int(x)));

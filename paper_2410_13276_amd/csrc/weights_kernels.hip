@@ -75,6 +75,9 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
   constexpr int SUB = S::SUB, KT = S::KT, ROWS = S::ROWS, STEPS = S::STEPS, NGX = S::NGX;
   constexpr int RV = 4 / PACK;                  // rows whose scores a lane holds
   constexpr int NPH = Q4 ? NG / PACK : 1;
+  // as in q4_attn_kernels.hip: the channels of one group a step
+  constexpr bool ALIGNED = NPH > 1;
+  static_assert(!ALIGNED || PACK == 1, "a block's groups all share the rows, or none");
   constexpr int KW = Q4 ? D / 32 : 4 * STEPS;   // dwords of a key per lane
   extern __shared__ __attribute__((aligned(16))) char room[];
   __shared__ __attribute__((aligned(16))) float sks[kWaves][Q4 ? KT : 1][NGX], skm[kWaves][Q4 ? KT : 1][NGX];
@@ -260,8 +263,9 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
         }
         bf16x8 parts[QP];
         split<QP>(y, parts);
-        // 4 bits: lane 16 j + row holds elements D / 4 j ..; else, of step i, elements 32 i + 8 j ..
-        const int step = Q4 ? piece % STEPS : piece / 4, lane_j = Q4 ? piece / STEPS : piece % 4;
+        // keys' quarters as they are: lane 16 j + row holds elements D / 4 j ..; else, of step i, elements 32 i + 8 j ..
+        constexpr bool QUARTERS = Q4 && !ALIGNED;
+        const int step = QUARTERS ? piece % STEPS : piece / 4, lane_j = QUARTERS ? piece / STEPS : piece % 4;
 #pragma unroll
         for (int part = 0; part < QP; ++part)
 #pragma unroll
@@ -273,7 +277,6 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
     }
   };
 
-  const int quad_group = j * NGX / 4;
   while (x < x_end) {
     // ---- a run of one head's units [u0, u1)
     const int u1 = min(row_units, u0 + (x_end - x));
@@ -299,6 +302,9 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
           skm[wave][lane][g] = __uint_as_float(kpq[g] & 0xffff0000u);
         }
         __builtin_amdgcn_wave_barrier();
+        if constexpr (ALIGNED)
+#pragma unroll
+          for (int i = 0; i < SUB; ++i) by_channels(kq[i]);
       }
       float sum[SUB];
 #pragma unroll
@@ -316,9 +322,6 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
           if constexpr (Q4) {
 #pragma unroll
             for (int ph = 0; ph < NPH; ++ph) {
-              uint32_t own = quad_group == ph ? ~0u : 0u;
-              int at = lane;
-              if constexpr (NPH > 1) asm volatile("" : "+v"(own), "+v"(at));  // (Q is read and masked here each time: kept, it would spill)
               f32x4 y[SUB], all;
 #pragma unroll
               for (int r = 0; r < 4; ++r) {
@@ -328,16 +331,13 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
                 for (int i = 0; i < SUB; ++i) y[i][r] = -kMid * q2.x;
               }
 #pragma unroll
-              for (int f = 0; f < STEPS; ++f) {
+              for (int f = ph * (STEPS / NPH); f < (ph + 1) * (STEPS / NPH); ++f) {
                 bf16x8 k8[SUB];
 #pragma unroll
                 for (int i = 0; i < SUB; ++i) k8[i] = open8(kq[i][f]);
 #pragma unroll
                 for (int part = QP - 1; part >= 0; --part) {
-                  u32x4 q = sq[cb - cb0][part][f][at];
-                  if constexpr (NPH > 1)
-#pragma unroll
-                    for (int z = 0; z < 4; ++z) q[z] &= own;
+                  const u32x4 q = sq[cb - cb0][part][f][lane];
 #pragma unroll
                   for (int i = 0; i < SUB; ++i)
                     y[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, q), k8[i], y[i], 0, 0, 0);
