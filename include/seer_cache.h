@@ -71,7 +71,8 @@ typedef struct {
  * Token (b, s) of k and v goes to slot positions[b][s] of the sequence of table row rows[b][s]
  * (rows NULL: row b), in 4 bits.  rope (NULL: none) rotates k first, at position rope_positions[b][s] (NULL:
  * positions[b][s]), in fp32, and the rotated values are held without a rounding in between.  Padding, and what
- * is left as it is, as in seer_kv_append.
+ * is left as it is, as in seer_kv_append; two tokens of a call may not go to the same slot (its codes may be of one
+ * and its params of the other then).
  * SEER_ERR_INVALID_ARG: a cache of group 0 (seer_kv_append serves it).
  * SEER_ERR_UNSUPPORTED: as seer_kv_append, and a group that head_dim is no multiple of or that is not 32 or 64.
  */
@@ -83,7 +84,7 @@ seer_status seer_kv_append_q4(const seer_kv_cache* cache, const seer_kv_tokens* 
  * What the cache holds for token (b, s), at slot positions[b][s] of the sequence of table row rows[b][s] (rows
  * NULL: row b), to k and v (desc: their layout and type; of a cache of group 0, its type).  The value of a code is
  * formed in fp32 (one rounding) and rounded to the type.  Tokens whose position or row is negative or beyond the table, or
- * whose page is none, read as 0.  k and v may not overlap the pools.
+ * whose page is none, read as 0.  k and v may not overlap the pools or each other.
  * SEER_ERR_UNSUPPORTED: as seer_kv_append.
  */
 seer_status seer_kv_read(const seer_kv_cache* cache, const seer_kv_tokens* desc, void* k, void* v,
@@ -144,7 +145,7 @@ typedef struct {
   int32_t batch;                  /* sequences: table rows 0 .. batch - 1 */
   int32_t keep, first, last;      /* slots to keep, the first and last ones among them; first + last <= keep >= 1 */
   const int32_t* lengths;         /* device [batch]: slots in use */
-  int32_t* new_lengths;           /* device [batch] */
+  int32_t* new_lengths;           /* device [batch]; may be `lengths` */
   const int32_t* new_table;       /* device [batch][new_max_pages]: pages (of the same pools) that the kept slots go to */
   int64_t new_table_stride;
   int32_t new_max_pages;          /* page_size new_max_pages >= keep */

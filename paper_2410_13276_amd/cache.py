@@ -59,12 +59,17 @@ class Q4Pool:
                 or ps[3] != 2 and pn[3] > 1 or (ps[0] | ps[1] | ps[2]) & 1 or params.get_device() != dev
                 or codes.dtype is not t.uint8 or params.dtype is not t.bfloat16):
             self._refuse(codes, params)
-        self.codes, self.params = codes, params
         dim = 2 * cn[3]
-        self.shape = (cn[0], cn[1], cn[2], dim)  # [pages, heads_kv, page_size, head_dim]
-        self.group = dim // pn[3]
-        self._strides = (cs[0], cs[1], cs[2], ps[0] // 2, ps[1] // 2, ps[2] // 2)
-        self._dev = dev
+        put = super().__setattr__
+        put("codes", codes)
+        put("params", params)
+        put("shape", (cn[0], cn[1], cn[2], dim))  # [pages, heads_kv, page_size, head_dim]
+        put("group", dim // pn[3])
+        put("_strides", (cs[0], cs[1], cs[2], ps[0] // 2, ps[1] // 2, ps[2] // 2))
+        put("_dev", dev)
+
+    def __setattr__(self, name, value):
+        raise AttributeError("a Q4Pool's tensors are given when it is made")
 
     @staticmethod
     def _refuse(c, p):
@@ -359,7 +364,7 @@ def kv_evict(k_cache, v_cache, table, lengths, weights, new_table, keep: int, *,
     """Cuts every sequence to `keep` slots of each KV head, which go to the pages of new_table (seer_kv_evict): its `first`
     first and `last` last ones, and of the others those of the largest weight, equal ones in their order.  lengths: int32
     [B], slots in use; weights: float32 [B, Hkv, W].  The pages of new_table may not be ones that the table's rows hold.
-    out: (lengths int32 [B], kept int32 [B, Hkv, keep], weights float32 [B, Hkv, W' >= keep]) to write to, the latter with 0
+    out: (lengths int32 [B], which may be `lengths`, kept int32 [B, Hkv, keep], weights float32 [B, Hkv, W' >= keep]) to write to, the latter with 0
     behind the kept slots' weights; None: new ones, W' what new_table has room for.  Returns them; kept says which slots
     they were (-1 where a sequence had fewer)."""
     if _d._t is None:

@@ -103,11 +103,9 @@ __device__ __forceinline__ Row row_of(const PickArgs& ka, int pair) {
   r.want = r.n > a.keep ? a.keep - a.first - a.last : 0;
   return r;
 }
-// What needs no choice: the length, the slots that always stay, and what is behind them.
-__device__ __forceinline__ void write_rest(const PickArgs& ka, const Row& r, int pair, int tid) {
+// What needs no choice: the slots that always stay, and what is behind them.
+__device__ __forceinline__ void write_rest(const PickArgs& ka, const Row& r, int tid) {
   const EvictArgs& a = ka.a;
-  const int b = pair / (uint32_t)a.cache.heads_kv;
-  if (pair == b * a.cache.heads_kv && tid == 0) a.new_lengths[b] = r.taken;
   for (int64_t i = r.taken + tid; i < a.new_width; i += kThreads) r.new_weights[i] = 0.f;
   for (int64_t i = r.taken + tid; i < a.keep; i += kThreads) r.kept[i] = -1;
   auto keep_slot = [&](int to, int slot) {
@@ -205,7 +203,7 @@ __global__ __launch_bounds__(kThreads) void evict_pick_kernel(PickArgs ka) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const Row r = row_of(ka, blockIdx.x);
   Slots<EL> slots(r, ka.a.width, r.lo, r.want ? r.hi : r.lo, wave, lane);
-  write_rest(ka, r, blockIdx.x, tid);
+  write_rest(ka, r, tid);
   if (r.want == 0) return;
   Known k = {0, r.want};
 #pragma unroll 1
@@ -224,7 +222,7 @@ __global__ __launch_bounds__(kThreads) void evict_part_kernel(PickArgs ka) {
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int part = blockIdx.x, pair = blockIdx.y;
   const Row r = row_of(ka, pair);
-  if (DIGIT == 3 && part == 0) write_rest(ka, r, pair, tid);
+  if (DIGIT == 3 && part == 0) write_rest(ka, r, tid);
   if (r.want == 0) return;
   // (parts as long as this row asks for)
   const int each = max(kPart, (r.hi - r.lo + ka.parts - 1) / ka.parts);
@@ -282,16 +280,21 @@ __global__ __launch_bounds__(kThreads) void evict_part_kernel(PickArgs ka) {
 struct MoveArgs {
   EvictArgs a;
   int64_t entries;  // batch heads_kv keep
+  int capacity;
   int64_t ksp, ksh, kss, vsp, vsh, vss;  // strides in bytes
 };
 
-// LANES threads move an entry, each 16 bytes of its key and of its value; PARAMS: and a dword of their params.
+// LANES threads move an entry, each 16 bytes of its key and of its value; PARAMS: and a dword of their params.  (There are more
+// threads than sequences.)
 // PAST: past the caches, which pays where more is moved than they hold (168 MB of 4 bits 70.7 -> 57.6 us, 17 MB of bf16 7.7 -> 9.1).
 template <int LANES, int PARAMS, bool PAST>
 __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs ka) {
   const EvictArgs& a = ka.a;
   const int piece = threadIdx.x % LANES;
   const uint32_t keep = a.keep, heads = a.cache.heads_kv;
+  // the lengths, which may be written in place: the launches that read the old ones have ended
+  if (const int64_t b = (int64_t)blockIdx.x * 256 + threadIdx.x; b < a.batch)
+    a.new_lengths[b] = min(min(max(a.lengths[b], 0), ka.capacity), a.keep);
   auto fetch = [](const char* p) -> u32x4 {
     if constexpr (PAST) return __builtin_nontemporal_load((const u32x4*)p);
     else return *(const u32x4*)p;
@@ -367,7 +370,7 @@ hipError_t launch_evict(const EvictArgs& a, hipStream_t s) {
   if (e != hipSuccess) return e;
   const int size = a.cache.group ? 1 : a.bf16 ? 2 : 4;
   const PoolView &kc = a.cache.k, &vc = a.cache.v;
-  const MoveArgs m = {a, pairs * a.keep, kc.sp * size, kc.sh * size, kc.ss * size, vc.sp * size, vc.sh * size, vc.ss * size};
+  const MoveArgs m = {a, pairs * a.keep, capacity, kc.sp * size, kc.sh * size, kc.ss * size, vc.sp * size, vc.sh * size, vc.ss * size};
   if (!a.cache.group) {
     const int bytes = a.cache.head_dim * size;
     return bytes == 512 ? move<32, 0>(m, s) : bytes == 256 ? move<16, 0>(m, s) : move<8, 0>(m, s);

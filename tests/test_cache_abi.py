@@ -247,3 +247,10 @@ def test_pools_are_checked():
                           (kc.codes[..., ::2], kc.params), (kc.codes, kc.params[..., :1, :1])):
         with pytest.raises(ValueError):
             seer.Q4Pool(codes, params)
+
+
+def test_a_pool_keeps_its_tensors():
+    kc, _ = seer.alloc_kv_cache_q4(4, 16, 2, 64, device="cpu")
+    for name, value in (("codes", kc.codes), ("params", kc.params), ("group", 64)):
+        with pytest.raises(AttributeError):
+            setattr(kc, name, value)

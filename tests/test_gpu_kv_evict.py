@@ -134,3 +134,50 @@ def test_lengths_out_of_range_and_holes():
     assert n.tolist() == [0, 6] and kept[0, 0].tolist() == [-1] * 6
     assert kept[1, 0].tolist() == R.evict(w.cpu(), [0, 16], 6, 0, 2, 16)[1][0]
     assert torch.equal(kc[5, 0, :6], torch.cat((kc[2, 0], kc[3, 0]))[kept[1, 0].long()])
+
+
+@pytest.mark.parametrize("n", [300, 40000])
+def test_lengths_in_place(n):
+    """New lengths over the old ones, short rows (a workgroup each) and long ones (several)."""
+    gen = torch.Generator().manual_seed(n)
+    table, pages, free = R.paged(gen, [n, n, n], 64, spare=6)
+    to = torch.tensor(free[:6], dtype=torch.int32).reshape(3, 2).cuda()
+    kc, vc = (torch.randn(pages, 2, 64, 64, generator=gen).to(torch.bfloat16).cuda() for _ in range(2))
+    w = torch.rand(3, 2, n, generator=gen)
+    lengths = [n, 90, n - 1]
+    n32 = torch.tensor(lengths, dtype=torch.int32).cuda()
+    out = (n32, torch.empty(3, 2, 100, dtype=torch.int32).cuda(), torch.empty(3, 2, 100).cuda())
+    back, kept, _ = seer.kv_evict(kc, vc, table.cuda(), n32, w.cuda(), to, 100, first=2, last=5, out=out)
+    assert back is n32 and n32.tolist() == [100, 90, 100]
+    for b, x in enumerate(R.evict(w, lengths, 100, 2, 5, table.shape[1] * 64)):
+        for h in range(2):
+            assert kept[b, h].tolist() == x[h] + [-1] * (100 - len(x[h]))
+
+
+@pytest.mark.parametrize("kind,B,keep", [("bf16", 4, 4200), ("q4", 8, 8200)])
+def test_large_moves(kind, B, keep):
+    """More than the caches hold."""
+    gen = torch.Generator().manual_seed(B)
+    H, page, n = 8, 64, keep + 100
+    table, pages, free = R.paged(gen, [n] * B, page, spare=B * (-(-keep // page)))
+    table, to = table.cuda(), torch.tensor(free, dtype=torch.int32)[:B * (-(-keep // page))].reshape(B, -1).cuda()
+    if kind == "q4":
+        kc, vc = seer.alloc_kv_cache_q4(pages, page, H, 128)
+        for p in (kc, vc):
+            p.codes.random_(0, 256)
+            p.params.copy_(torch.rand(p.params.shape, device="cuda"))
+        planes_of = (kc.codes, kc.params, vc.codes, vc.params)
+    else:
+        kc, vc = planes_of = [torch.rand(pages, H, page, 128, device="cuda").to(torch.bfloat16) for _ in range(2)]
+    w = torch.rand(B, H, n, generator=gen).cuda()
+    old = [p.clone() for p in planes_of]
+    n32 = torch.full((B,), n, dtype=torch.int32).cuda()
+    _, kept, new_w = seer.kv_evict(kc, vc, table, n32, w, to, keep)
+    want = w.sort(dim=2, descending=True, stable=True).indices[..., :keep].sort(dim=2).values  # (of equal ones the lower slot)
+    assert torch.equal(kept.long(), want)
+    assert torch.equal(new_w[:, :, :keep], w.gather(2, want))
+    i, h = torch.arange(keep).cuda(), torch.arange(H).cuda()[None, :, None]
+    src = table.long().gather(1, (want // page).reshape(B, -1)).reshape(B, H, keep)
+    dst = to.long()[:, i // page][:, None].expand(B, H, keep)
+    for a, p in zip(old, planes_of):
+        assert torch.equal(p[dst, h, i % page], a[src, h, want % page])

@@ -179,3 +179,19 @@ def test_fp32_precision():
     off = float((o.cpu().double() - ro).norm() / ro.norm())
     print("off by", off)
     assert off < 2e-6
+
+
+def test_many_sequences():
+    """More sequences than a wavefront has lanes, most of them empty."""
+    gen = torch.Generator().manual_seed(40)
+    lengths = [1, 700, 2, 0, 0, 33] + [0] * 150 + [64, 1]
+    pos = torch.tensor(lengths, dtype=torch.int32)[:, None] - 1
+    table, pages, _ = R.paged(gen, lengths, 16, wide=50)
+    kc, vc = (R.random_pool(seer, gen, pages, 2, 16, 64, 32) for _ in range(2))
+    q = torch.randn(len(lengths), 4, 1, 64, generator=gen).to(torch.bfloat16)
+    o, lse = seer.paged_attn_q4(q.cuda(), kc, vc, table.cuda(), pos.cuda(), want_lse=True)
+    ro, rl, eo, el = R.attend(q, kc, vc, table, 16, pos, 0.0, None)
+    none = pos.expand(-1, 4)[..., None] < 0
+    assert torch.equal(lse.cpu() == -math.inf, none) and not bool(o.cpu()[none.squeeze(-1)].any())
+    assert bool(((lse.cpu().double() - rl).abs()[~none] <= (el + R.U * rl.abs())[~none]).all())
+    assert_rounded(o, ro, eo, "o")

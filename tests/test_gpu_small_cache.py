@@ -88,19 +88,20 @@ def test_a_prompt_its_eviction_and_the_answer(kind):
         assert bool(((w2.cpu().double() - ref).abs() <= err).all())
 
 
-def test_a_captured_step():
+@pytest.mark.parametrize("room", [640, 40000])
+def test_a_captured_step(room):
     """A step of generation and an eviction in a graph, replayed with new tokens, positions and lengths, with eager work in
     between: every replay is the eager result, bit for bit."""
     gen = torch.Generator().manual_seed(2)
     B, Hq, Hkv, D, page = 3, 8, 2, 64, 16
-    table, pages, free = R.paged(gen, [640, 640, 640], page, spare=12)
+    table, pages, free = R.paged(gen, [room] * 3, page, spare=12)
     table, to = table.cuda(), torch.tensor(free[:12], dtype=torch.int32).reshape(3, 4).cuda()
     f = freqs(D).cuda()
 
     def state():
         g = torch.Generator().manual_seed(3)
         kc, vc = (R.random_pool(seer, g, pages, Hkv, page, D, 32) for _ in range(2))
-        return kc, vc, torch.rand(B, Hkv, 640, generator=g).cuda()
+        return kc, vc, torch.rand(B, Hkv, room, generator=g).cuda()
 
     def step(kc, vc, w, k1, v1, q1, slots, n):
         seer.kv_append_q4(k1, v1, kc, vc, table, slots, inv_freq=f)
@@ -112,8 +113,8 @@ def test_a_captured_step():
     def draw(i):
         g = torch.Generator().manual_seed(100 + i)
         x = [torch.randn(B, h, D, generator=g).to(torch.bfloat16).cuda() for h in (Hkv, Hkv, Hq)]
-        slots = torch.randint(0, 640, (B,), generator=g).to(torch.int32).cuda()
-        return (*x, slots, torch.randint(0, 641, (B,), generator=g).to(torch.int32).cuda())
+        slots = torch.randint(0, room, (B,), generator=g).to(torch.int32).cuda()
+        return (*x, slots, torch.randint(0, room + 1, (B,), generator=g).to(torch.int32).cuda())
 
     mine, other = state(), state()
     args = draw(0)
