@@ -30,6 +30,12 @@
 // Precision: fp32 statistics and sums.  A q that is rotated here, or fp32, enters in three bf16 parts, which hold fp32 whole (two,
 // rounded to nearest, left the log-sum-exp 1e-6 of itself off where this leaves 1e-7), and so does p step where the output is
 // fp32; where it is bf16, in two, 2^-18 of it off at most, where the output's own rounding is 2^-9.
+//
+// Measured (bf16, one MI355X): 32 / 8 heads of 128 in groups of 32, a token after 131072 tokens 39 us + 4 of the join, for 168 MB
+// (4.2e12 bytes a second while it runs; a kernel that only reads reaches 6.2e12); 64 sequences of 200 to 16000 tokens 73 + 4.5 for 285
+// MB.  What bounds it is latency: a wavefront has one tile, 10 KB, in flight, two a SIMD, and its registers are used up (a second
+// tile spills: 79 us); the vector units issue a third of the time, the matrix units a quarter.  About 9 us are a run's beginning (positions, table,
+// tile, one after the other) and end.  With 16 rows and more the vector units decide: four groups' factors and weights a tile.
 #include <algorithm>
 #include <type_traits>
 
@@ -44,7 +50,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kKeys = 64;      // of a tile
-constexpr int kWholeKeys = 512;  // rows with room for so many are not split
+// Rows with room for so many keys are not split, which saves the joining launch (32 / 8 heads of 128, 500 keys in room for 512: a
+// sequence 9.3 us against 12.6 split, 64 of them 13.8 against 15.3; 1000 in 1024: a sequence 13.2 whole, 12.6 split).
+constexpr int kWholeKeys = 512;
 
 struct PoolStrides {  // of codes in 16-byte pieces, of params in rows of them
   uint32_t page, slot, ppage, pslot;
@@ -96,7 +104,7 @@ __device__ __forceinline__ float row_sum(float x) {
 // D: elements of a head.  NG: groups of a head.  PACK: of them, those that share the columns.  QP: bf16 parts of q (1: bf16
 // as it is, 3: rotated, or fp32).
 // RUN: pages hold whole aligned runs of 16
-// keys, whose rows lie within 2^30 bytes.
+// keys, whose rows lie within 2^30 bytes (a token after 131072 tokens: 42 us; with pages of 24, looked up key by key, see the rule in launch).
 template <typename T, int D, int NG, int PACK, int QP, bool RUN>
 __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   constexpr int ROWS = 16 / PACK, NPH = NG / PACK;

@@ -20,8 +20,6 @@ namespace seer {
 
 namespace {
 
-constexpr int kThreads = 512;
-constexpr int kWaves = kThreads / kWave;
 constexpr int kRoom = 72 << 10;  // bytes of LDS for rows: two workgroups of a CU hold the rows of 64 tokens of 4 heads of 128 each
 
 struct KernelArgs {
@@ -65,12 +63,18 @@ struct Shape {
   // of a block: the operand as the lanes read it, rows, cosines and sines of their tokens
   static constexpr int OPERAND = QP * STEPS * kWave * 16;
   static constexpr int BYTES = OPERAND + ROWS * (int)sizeof(Row) + (TURNS ? ROWS * (D / 2) * 8 : 0);
-  static constexpr int WAVES = !Q4 || PACK > 1 || NG == 1 ? 4 : 2;  // per SIMD, as the registers allow
+  // per SIMD, as the registers allow (4 bits of 128 elements with q in three parts: 4 spill 26, and a token after 131072 takes 39.5
+  // us for 27.1)
+  static constexpr int WAVES = !Q4 || NG == 1 ? 4 : PACK == 1 ? 2 : D == 128 && QP == 3 ? 3 : 4;
+  // few rows: small workgroups, whose shares are finer (64 sequences of 200 tokens 12.8 -> 8.2 us); many: large ones, which share them
+  static constexpr int THREADS = Q4 && PACK > 1 ? 256 : 512;
+  static constexpr int UNIT_SHIFT = (THREADS == 512 ? 3 : 2) + (F32 ? 5 : 6);  // log2 of a tile for each wavefront
 };
 
 template <typename T, int D, int NG, int PACK, int QP, bool RUN>
-__global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void weights_kernel(KernelArgs ka) {
+__global__ __launch_bounds__((Shape<T, D, NG, PACK, QP>::THREADS), (Shape<T, D, NG, PACK, QP>::WAVES)) void weights_kernel(KernelArgs ka) {
   using S = Shape<T, D, NG, PACK, QP>;
+  constexpr int kThreads = S::THREADS, kWaves = kThreads / kWave;
   constexpr bool BF = S::BF, Q4 = S::Q4, F32 = S::F32;
   constexpr int SUB = S::SUB, KT = S::KT, ROWS = S::ROWS, STEPS = S::STEPS, NGX = S::NGX;
   constexpr int RV = 4 / PACK;                  // rows whose scores a lane holds
@@ -448,14 +452,19 @@ __global__ __launch_bounds__(kThreads, (Shape<T, D, NG, PACK, QP>::WAVES)) void 
 }
 
 template <typename T, int D, int NG, int PACK, int QP>
-hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
+hipError_t launch(KernelArgs& k, hipStream_t s) {
   using S = Shape<T, D, NG, PACK, QP>;
+  constexpr int kWaves = S::THREADS / kWave;
+  k.unit_shift = S::UNIT_SHIFT;
+  const int64_t heads = (int64_t)k.a.q.batch * k.a.q.cache.heads_kv;
+  auto units = [&]() -> int64_t { return ((int64_t)k.capacity + ((int64_t)1 << k.unit_shift) - 1) >> k.unit_shift; };
+  while ((units() + 1) * heads > (1 << 30)) ++k.unit_shift;
   k.blocks = (k.rows + S::ROWS - 1) / S::ROWS;
   k.held = std::min(k.blocks, std::max(1, kRoom / S::BYTES));
   // as many workgroups as the GPU holds at once: by registers, and by the LDS
   const int lds = k.held * S::BYTES + (S::Q4 ? kWaves * S::KT * NG * 8 : 0);
   const int per_cu = std::max(1, std::min(S::WAVES * 4 / kWaves, (160 << 10) / (lds + 1024)));
-  const dim3 grid((unsigned)std::min((int64_t)256 * per_cu, units));
+  const dim3 grid((unsigned)std::min((int64_t)256 * per_cu, units() * heads));
   const size_t room = (size_t)k.held * S::BYTES;
   const int64_t far = (int64_t)1 << 26;  // (the 16 rows of a run within 2^30 bytes)
   auto kernel = k.a.q.cache.table.page.d % 16 == 0 && k.kss < far ? weights_kernel<T, D, NG, PACK, QP, true>
@@ -464,25 +473,25 @@ hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
     const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
     if (e != hipSuccess) return e;
   }
-  kernel<<<grid, kThreads, room, s>>>(k);
+  kernel<<<grid, S::THREADS, room, s>>>(k);
   return hipGetLastError();
 }
 template <typename T, int D, int NG, int PACK>
-hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
-  if constexpr (sizeof(T) == 4) return launch<T, D, NG, PACK, NG == 0 ? 1 : 3>(k, units, s);
-  else return k.a.q.rope.freq ? launch<T, D, NG, PACK, 3>(k, units, s) : launch<T, D, NG, PACK, 1>(k, units, s);
+hipError_t launch(KernelArgs& k, hipStream_t s) {
+  if constexpr (sizeof(T) == 4) return launch<T, D, NG, PACK, NG == 0 ? 1 : 3>(k, s);
+  else return k.a.q.rope.freq ? launch<T, D, NG, PACK, 3>(k, s) : launch<T, D, NG, PACK, 1>(k, s);
 }
 // (the groups share the operand's rows where these leave room for all of them)
 template <typename T, int D, int NG>
-hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
+hipError_t launch(KernelArgs& k, hipStream_t s) {
   if constexpr (NG > 1)
-    if (k.rows <= 16 / NG) return launch<T, D, NG, NG>(k, units, s);
-  return launch<T, D, NG, 1>(k, units, s);
+    if (k.rows <= 16 / NG) return launch<T, D, NG, NG>(k, s);
+  return launch<T, D, NG, 1>(k, s);
 }
 template <typename T, int D>
-hipError_t launch(KernelArgs& k, int64_t units, hipStream_t s) {
+hipError_t launch(KernelArgs& k, hipStream_t s) {
   const int group = k.a.q.cache.group;
-  return group == 0 ? launch<T, D, 0>(k, units, s) : group == 32 ? launch<T, D, D / 32>(k, units, s) : launch<T, D, D / 64>(k, units, s);
+  return group == 0 ? launch<T, D, 0>(k, s) : group == 32 ? launch<T, D, D / 32>(k, s) : launch<T, D, D / 64>(k, s);
 }
 
 }  // namespace
@@ -500,13 +509,9 @@ hipError_t launch_weights(const WeightArgs& a, hipStream_t s) {
   k.group = fast_div(group);
   k.rows = group * q.tokens;
   k.capacity = std::min(q.cache.table.max_pages * q.cache.table.page.d, a.width);
-  k.unit_shift = q4 || q.bf16 ? 9 : 8;  // a tile for each wavefront
-  const int64_t rows = (int64_t)q.batch * q.cache.heads_kv;
-  auto units = [&]() -> int64_t { return ((int64_t)k.capacity + ((int64_t)1 << k.unit_shift) - 1) >> k.unit_shift; };
-  while ((units() + 1) * rows > (1 << 30)) ++k.unit_shift;
   k.scale_log2 = q.scale * kLog2e * (q4 ? 16.f : 1.f);
-  if (q.bf16) return q.cache.head_dim == 128 ? launch<uint16_t, 128>(k, units() * rows, s) : launch<uint16_t, 64>(k, units() * rows, s);
-  return q.cache.head_dim == 128 ? launch<float, 128>(k, units() * rows, s) : launch<float, 64>(k, units() * rows, s);
+  if (q.bf16) return q.cache.head_dim == 128 ? launch<uint16_t, 128>(k, s) : launch<uint16_t, 64>(k, s);
+  return q.cache.head_dim == 128 ? launch<float, 128>(k, s) : launch<float, 64>(k, s);
 }
 
 }  // namespace seer
