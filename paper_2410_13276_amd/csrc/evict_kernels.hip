@@ -7,6 +7,10 @@
 // a digit adds them up (no atomics between workgroups); what the parts before a part write follows from
 // the histograms too.  A last launch moves the keys and values, 16 bytes a thread, whatever they are held as: the places it
 // writes are no places that it reads, so that it needs no order.
+//
+// Measured, one MI355X: 64 sequences of 1700 to 2400 slots cut to 2048 (8 heads of 128 in 4 bits) 15 us to choose, 57 to move 336 MB at
+// 5.9e12 bytes a second, the memory's rate; 131072 slots cut to 4096 (bf16) 41 us to choose, by launches and barriers (the weights are 4 MB), 7.5 to move 34 MB.
+// A row of 131072 slots by one workgroup a head takes 185 us to choose.
 #include <algorithm>
 
 #include "cache.h"
@@ -19,7 +23,9 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kBins = 2048;
-constexpr int kPart = 16384;  // slots of a part of a long row at least
+// slots of a part of a long row at least (131072 slots of 8 heads, the four launches together: 42 us; 8192 40 to 41, 4096 48, as each adds
+// up all parts' histograms)
+constexpr int kPart = 16384;
 // of a part in the workspace: three histograms; its slots above the weight by the first and second digit; (the first part's:)
 // the weight's upper bits and how many stay of those that have them, after the first and the second digit
 constexpr int kPartInts = 3 * kBins + 64;

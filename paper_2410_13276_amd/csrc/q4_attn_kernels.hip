@@ -24,18 +24,19 @@
 //
 // A wavefront takes 64 keys at a time.  K's codes come to registers as the operand wants them (16 bytes of one
 // key a lane); V's go through the wavefront's own LDS and come back transposed (ds_read_b64_tr_b4: 16 keys of
-// one channel a lane); so do both params.  Where pages hold whole aligned runs of 16 keys, a run's address is formed by the
-// scalar unit.
+// one channel a lane); so do both params.  Where pages hold whole aligned runs of 16 keys, a lane looks up a run's address
+// for all.
 //
 // Precision: fp32 statistics and sums.  A q that is rotated here, or fp32, enters in three bf16 parts, which hold fp32 whole (two,
 // rounded to nearest, left the log-sum-exp 1e-6 of itself off where this leaves 1e-7), and so does p step where the output is
 // fp32; where it is bf16, in two, 2^-18 of it off at most, where the output's own rounding is 2^-9.
 //
-// Measured (bf16, one MI355X): 32 / 8 heads of 128 in groups of 32, a token after 131072 tokens 39 us + 4 of the join, for 168 MB
-// (4.2e12 bytes a second while it runs; a kernel that only reads reaches 6.2e12); 64 sequences of 200 to 16000 tokens 73 + 4.5 for 285
+// Measured (bf16, one MI355X): 32 / 8 heads of 128 in groups of 32, a token after 131072 tokens 42 us + 4 of the join, for 168 MB
+// (4e12 bytes a second while it runs; a kernel that only reads reaches 6.2e12); 64 sequences of 200 to 16000 tokens 77 + 4.5 for 285
 // MB.  What bounds it is latency: a wavefront has one tile, 10 KB, in flight, two a SIMD, and its registers are used up (a second
-// tile spills: 79 us); the vector units issue a third of the time, the matrix units a quarter.  About 9 us are a run's beginning (positions, table,
-// tile, one after the other) and end.  With 16 rows and more the vector units decide: four groups' factors and weights a tile.
+// tile spills: 79 us); the vector units issue 0.46 of the time, the matrix units work 0.2.  About 9 us are a run's beginning (positions, table,
+// tile, one after the other) and end.  With 16 rows and more a tile's own chain is what takes long, scores, weights and factors of two or
+// four phases: 28 rows of 4 heads over 93643 tokens in groups of 64 46 us for 54 MB.
 #include <algorithm>
 #include <type_traits>
 
@@ -104,7 +105,8 @@ __device__ __forceinline__ float row_sum(float x) {
 // D: elements of a head.  NG: groups of a head.  PACK: of them, those that share the columns.  QP: bf16 parts of q (1: bf16
 // as it is, 3: rotated, or fp32).
 // RUN: pages hold whole aligned runs of 16
-// keys, whose rows lie within 2^30 bytes (a token after 131072 tokens: 42 us; with pages of 24, looked up key by key, see the rule in launch).
+// keys, whose rows lie within 2^30 bytes (a token after 131072 tokens: 50 us a call, pages of 64 and of 24, which
+// are looked up key by key, alike; pages of 1 82).
 template <typename T, int D, int NG, int PACK, int QP, bool RUN>
 __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   constexpr int ROWS = 16 / PACK, NPH = NG / PACK;
@@ -697,7 +699,8 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   }
 }
 
-// Columns that are shared by groups, rows of a block.
+// Groups that share the columns: as many as the rows leave room for, since each phase opens and weighs the tile again (8 x 8192 tokens in groups
+// of 32: 8 rows of each of 8 heads, two phases, 36 us; 16 rows of each of 4, four phases, half the tiles, 37).
 int pack_of(int groups, int rows) {
   int pack = groups;
   while (pack > 1 && rows > 16 / pack) pack /= 2;
@@ -725,6 +728,7 @@ Plan plan(int batch, int heads_q, int heads_kv, int tokens, int head_dim, int el
 
 template <typename T, int D, int NG, int PACK, int QP>
 hipError_t launch(const KernelArgs& k, dim3 grid, hipStream_t s) {
+  // (key by key costs registers: 28 rotated rows spill 105 of them instead of 61)
   const int64_t far = (int64_t)1 << 26;  // (16 rows of a run within 2^30 bytes)
   const CacheArgs& ca = k.a.q.cache;
   if (ca.table.page.d % 16 == 0 && ca.k.ss < far && ca.v.ss < far) q4_attn_kernel<T, D, NG, PACK, QP, true><<<grid, kThreads, 0, s>>>(k);
