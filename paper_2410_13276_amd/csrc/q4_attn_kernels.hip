@@ -170,9 +170,9 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   }
   const int upto = wave_prefix(mine);
   const TurnRate rate = turn_rate(freq);
-  const int w = blockIdx.x;
   const Deal deal((uint32_t)(__builtin_amdgcn_readlane(upto, kWave - 1) * items), gridDim.x);
-  if (w >= (int)deal.workers) return;
+  if (blockIdx.x >= (uint32_t)deal.workers) return;
+  const int w = share_of(ca.k, a.batch, blockIdx.x, (int)deal.workers);
   int x = deal.first(w);
   const int x_end = deal.first(w + 1);
   const int owner_lane = (int)__popcll(__ballot(upto * items <= x));

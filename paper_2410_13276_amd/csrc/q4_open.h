@@ -1,6 +1,7 @@
 // q4_open.h -- codes of 4 bits as operands of a matrix product.
 #pragma once
 
+#include "cache.h"
 #include "paged_common.h"
 
 namespace seer {
@@ -55,6 +56,17 @@ __device__ __forceinline__ void by_channels(uint32_t (&x)[N]) {
   } else {
     swap32(x[0], x[1]);
   }
+}
+
+// The share of workgroup `id` of `workers`.  Where pages are token-major, heads' codes share lines; with some sequences, successive
+// shares go to one XCD then (workgroups go round the 8 XCDs), so that a sequence's heads meet in its L2.  Token-major, 32 / 8 heads of
+// 128: 64 sequences of 3000 tokens attention 118 -> 77 us, weights 60 -> 49, 8 of 16000 56 -> 55 and 46 -> 39.5, 4 of 3000 (4 tokens each) 33 ->
+// 28; one sequence of 131072 72 -> 86 and 32 -> 50 (its heads' shares lie apart by multiples of 8 anyhow).  Head-major, 28 rows of 4 heads over 8 x 4096
+// tokens 35 -> 40.
+__device__ __forceinline__ int share_of(const PoolView& k, int batch, int id, int workers) {
+  if (k.sh >= k.ss || batch < 4) return id;
+  const int xcd = id % 8, each = workers / 8;
+  return xcd * each + min(xcd, workers % 8) + id / 8;
 }
 
 template <int CTRL>

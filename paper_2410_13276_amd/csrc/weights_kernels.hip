@@ -115,9 +115,9 @@ __global__ __launch_bounds__((Shape<T, D, NG, PACK, QP>::THREADS), (Shape<T, D, 
   const int upto = wave_prefix(mine);
   const TurnRate rate = turn_rate(freq);
   const uint32_t total = (uint32_t)(__builtin_amdgcn_readlane(upto, kWave - 1) * items);
-  const int w = blockIdx.x;
-  if ((uint32_t)w >= total) return;  // (a unit each at least, or none)
+  if (blockIdx.x >= total) return;  // (a unit each at least, or none)
   const Deal deal(total, gridDim.x);
+  const int w = share_of(ca.k, a.batch, blockIdx.x, (int)min(gridDim.x, total));
   int x = deal.first(w);
   const int x_end = deal.first(w + 1);
   const int owner_lane = (int)__popcll(__ballot(upto * items <= x));

@@ -149,3 +149,11 @@ def test_weights_sum_to_the_rows(kind):
     w = torch.zeros(2, 2, table.shape[1] * 16).cuda()
     seer.kv_weights(q, kc, table.cuda(), pos, lse, w, inv_freq=f)
     assert bool(((w.sum(-1) - 12).abs() < 12 * 2e-5).all())
+
+
+@pytest.mark.parametrize("kind", ["q4", "bf16"])
+@pytest.mark.parametrize("lengths", [[900, 3, 64, 700, 1300], [40] * 4, [1, 2000, 0, 1, 1, 600, 600, 90, 5000]])
+def test_token_major_batches(kind, lengths):
+    """Pages whose heads share lines, in numbers of sequences whose shares are ordered by XCD."""
+    gen = torch.Generator().manual_seed(len(lengths))
+    check(gen, torch.bfloat16, 8, 4, 128, 32, 64, lengths, kind=kind, order="pshd", wide=80)

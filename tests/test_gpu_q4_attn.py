@@ -195,3 +195,10 @@ def test_many_sequences():
     assert torch.equal(lse.cpu() == -math.inf, none) and not bool(o.cpu()[none.squeeze(-1)].any())
     assert bool(((lse.cpu().double() - rl).abs()[~none] <= (el + R.U * rl.abs())[~none]).all())
     assert_rounded(o, ro, eo, "o")
+
+
+@pytest.mark.parametrize("lengths", [[900, 3, 64, 700, 1300], [40] * 4, [1, 2000, 0, 1, 1, 600, 600, 90, 5000]])
+def test_token_major_batches(lengths):
+    """Pages whose heads share lines, in numbers of sequences whose shares are ordered by XCD."""
+    gen = torch.Generator().manual_seed(len(lengths))
+    check(gen, torch.bfloat16, 8, 4, 128, 32, 64, lengths, order="pshd", wide=80)
