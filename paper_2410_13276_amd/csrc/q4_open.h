@@ -20,6 +20,17 @@ __device__ __forceinline__ bf16x8 open8(uint32_t w) {
   return __builtin_bit_cast(bf16x8, y);
 }
 
+// The same less 1.5, exactly: for results in fp32, whose sums would carry the rounding of numbers 3 to 7 times the values'.
+__device__ __forceinline__ bf16x8 open8_centred(uint32_t w) {
+  u32x4 y = __builtin_bit_cast(u32x4, open8(w));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float lo = __uint_as_float(y[i] << 16) - 1.5f, hi = __uint_as_float(y[i] & 0xffff0000u) - 1.5f;
+    y[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+  }
+  return __builtin_bit_cast(bf16x8, y);
+}
+
 // x as the sum of N bf16 parts: three hold fp32 exactly (8 significant bits each time); two, each rounded to nearest, are
 // 2^-18 off at most.
 template <int N>

@@ -471,7 +471,7 @@ hipError_t launch(KernelArgs& k, hipStream_t s) {
   const dim3 grid((unsigned)std::min((int64_t)256 * per_cu, units() * heads));
   const size_t room = (size_t)k.held * S::BYTES;
   // whole aligned runs of 16 keys, their rows within 2^30 bytes, are looked up once (a rotated token after 131072 tokens: pages of 64
-  // and 16 39 us, pages of 24, key by key, 62)
+  // and 16 27 us, pages of 24, key by key, 29)
   const int64_t far = (int64_t)1 << 26;
   auto kernel = k.a.q.cache.table.page.d % 16 == 0 && k.kss < far ? weights_kernel<T, D, NG, PACK, QP, true>
                                                                  : weights_kernel<T, D, NG, PACK, QP, false>;
