@@ -88,8 +88,8 @@ hipError_t launch_paged_attn(const PagedArgs& a, hipStream_t s);
 size_t paged_attn_workspace(int batch, int heads_q, int heads_kv, int tokens, int head_dim);
 
 #ifdef __HIPCC__
-__device__ __forceinline__ int fast_quot(const FastDiv& f, int n) {
-  return (int)((__umulhi((uint32_t)n, f.m) + (uint32_t)n) >> f.s);
+__host__ __device__ __forceinline__ int fast_quot(const FastDiv& f, int n) {
+  return (int)(((uint32_t)((uint64_t)(uint32_t)n * f.m >> 32) + (uint32_t)n) >> f.s);
 }
 
 // A plane's angle per position as a fraction of a turn in 64-bit fixed point, within 2^-64 of a turn and 2^-52 of itself:

@@ -13,6 +13,12 @@ struct Stride16 {
 };
 
 #ifdef __HIPCC__
+// Where the page of the last of a run's keys [.., k_hi) stands in its table row, which look-ups of keys behind the run are
+// held to.  A run without keys is held to the first entry: the quotient of -1 is a large number (pages of 16: 268435455).
+__host__ __device__ __forceinline__ int last_page_of(const FastDiv& page, int k_hi) {
+  return fast_quot(page, k_hi > 0 ? k_hi - 1 : 0);
+}
+
 // The weights dealt to the workgroups: workgroup w has base (+ 1 for the first `rest`).  (All below 2^30: the
 // 64-bit divisions that this was first written with were 600 instructions at every workgroup's start.)
 struct Deal {

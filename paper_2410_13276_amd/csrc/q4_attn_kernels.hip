@@ -299,7 +299,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
     h = fast_quot(ka.blocks, item);
     key0 = (u0 << ka.unit_shift) + wave * kKeys;
     k_hi = u1 == row_units ? len : u1 << ka.unit_shift;
-    last_page = max(fast_quot(ca.table.page, k_hi - 1), 0);
+    last_page = last_page_of(ca.table.page, k_hi);
     kbase = (const char*)ca.k.data + h * ca.k.sh;
     vbase = (const char*)ca.v.data + h * ca.v.sh;
     kpbase = ca.k.params + h * ca.k.psh;
