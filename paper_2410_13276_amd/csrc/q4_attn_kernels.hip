@@ -13,8 +13,9 @@
 // for two codes.  The 1 is taken out again in fp32, at the sums' starting values, and half of the codes (4 of 8) enter
 // complemented, 1 + (15 - c) / 16, their factors negated: with u = 1.46875 = 1 + 7.5 / 16 either is u +- (c - 7.5) / 16, so that
 // what has to be taken out is u times a sum of terms of both signs, which stays as small as the result.  (All of one
-// sign, the second product's sums would be 5 to 100 times the result and carry their rounding into it.)  Where the output is fp32, 1.5 is
-// taken off each first, exactly (1000 keys of 64: o 1.2e-7 to 3.2e-7 off, and 6e-7 to 1e-6 without; 65536 tokens 30 -> 38 us).
+// sign, the second product's sums would be 5 to 100 times the result and carry their rounding into it.)  Where the output is fp32, codes
+// are looked up as (c - 7.5) / 16 instead, exactly, and nothing is taken out (1000 keys: o 1.6e-7 to 2.5e-7 off in the 2-norm, and 7e-7 to 1.1e-6
+// as above, 2e-6 to 3e-6 where one element of each group is far off; 65536 tokens of 32 / 8 heads of 128 34 us, and 30).
 //
 // Rows.  A step belongs to a group, so that a group's products may not run into another's sum.  Where a block has
 // few rows (16 / (D / group) at most), the 16 rows of the products' other operand are pairs of row and group: Q is 0 but in
@@ -119,11 +120,9 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   constexpr int PSTR = kKeys + 16 / RV;  // (rows of the weights fall on different banks)
   constexpr bool BF = sizeof(T) == 2;
   constexpr int PP = BF ? 2 : 3;       // bf16 parts of a weight times its step
-  // fp32: what a tile adds is formed by itself, from -MID times the sum of its factors on, and then added; bf16: the
-  // sums run on over the tiles, the factors' own beside them (its rounding, 2^-9, hides what that leaves)
+  // fp32: what a tile adds is formed by itself and then added; bf16: the sums run on over the tiles, the factors' own
+  // beside them (its rounding, 2^-9, hides what that leaves)
   constexpr bool RUNS = BF;
-  // (fp32: the codes are centred)
-  constexpr float MID = BF ? kMid : kMid - 1.5f;
   auto open = [](uint32_t codes) {
     if constexpr (BF) return open8(codes);
     else return open8_centred(codes);
@@ -401,7 +400,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const float2 y = sh.sum[RV * j + r / PACK][ph * PACK + r % PACK];
-        from[ph][r] = -MID * y.x;
+        from[ph][r] = BF ? -kMid * y.x : 0.f;
         all[ph][r] = y.y;
       }
 
@@ -411,7 +410,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
     float m[RV], l[RV], mids[NPH];
 #pragma unroll
     for (int v = 0; v < RV; ++v) m[v] = -INFINITY, l[v] = 0.f;
-    f32x4 offs[NPH];  // MID times the sum of the factors, in every element
+    f32x4 offs[NPH];  // (bf16) kMid times the sum of the factors, in every element
 #pragma unroll
     for (int ph = 0; ph < NPH; ++ph) {
       mids[ph] = 0.f;
@@ -419,7 +418,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
     }
     bf16x8 mid8;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) mid8[e] = (__bf16)(RUNS ? MID : -MID);
+    for (int e = 0; e < 8; ++e) mid8[e] = (__bf16)kMid;
 
     auto& st = sh.w[wave];
     for (; key0 < k_hi; key0 += STEP) {
@@ -471,7 +470,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
             const float2 q2 = sh.sum[at_row + r / PACK][ph * PACK + r % PACK];
             all_ph[r] = q2.y;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) y[i][r] = -MID * q2.x;
+            for (int i = 0; i < 4; ++i) y[i][r] = BF ? -kMid * q2.x : 0.f;
           }
         }
 #pragma unroll
@@ -590,7 +589,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
           const float x8[8] = {p[8 * f], p[8 * f + 4], p[8 * f + 1], p[8 * f + 5], p[8 * f + 2], p[8 * f + 6], p[8 * f + 3], p[8 * f + 7]};
           split<PP>(x8, pt[f]);
         }
-        if constexpr (!RUNS) offs[ph] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if constexpr (RUNS)
 #pragma unroll
         for (int part = PP - 1; part >= 0; --part)
 #pragma unroll
@@ -607,7 +606,7 @@ __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
             const i32x2 v = __builtin_amdgcn_ds_read_tr4_b64_v2i32((__attribute__((address_space(3))) i32x2*)row_at);
             v8[y][0] = open((uint32_t)v[0]);
             v8[y][1] = open((uint32_t)v[1]);
-            z[y] = RUNS ? acc[i + y] : offs[ph];
+            z[y] = RUNS ? acc[i + y] : f32x4{0.f, 0.f, 0.f, 0.f};
           }
 #pragma unroll
           for (int part = PP - 1; part >= 0; --part)

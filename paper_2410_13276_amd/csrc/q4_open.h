@@ -20,13 +20,21 @@ __device__ __forceinline__ bf16x8 open8(uint32_t w) {
   return __builtin_bit_cast(bf16x8, y);
 }
 
-// The same less 1.5, exactly: for results in fp32, whose sums would carry the rounding of numbers 3 to 7 times the values'.
+// The same codes as (c - 7.5) / 16, in the same order and with the same ones complemented: for results in fp32, whose sums would
+// carry the rounding of numbers 3 to 7 times the values'.  Sign and size of a code are its upper bit and the lower three, turned over
+// below the middle; the bytes of the 8 sizes are looked up, four codes at a time.
 __device__ __forceinline__ bf16x8 open8_centred(uint32_t w) {
-  u32x4 y = __builtin_bit_cast(u32x4, open8(w));
+  w ^= 0xffff0000u;
+  u32x4 y;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float lo = __uint_as_float(y[i] << 16) - 1.5f, hi = __uint_as_float(y[i] & 0xffff0000u) - 1.5f;
-    y[i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+  for (int odd = 0; odd < 2; ++odd) {
+    const uint32_t c = odd ? w >> 4 : w;
+    const uint32_t below = ~c & 0x08080808u;
+    const uint32_t size = (c ^ (below - (below >> 3))) & 0x07070707u;
+    const uint32_t lo = __builtin_amdgcn_perm(0xf0d0b090u, 0x6020c000u, size);
+    const uint32_t hi = __builtin_amdgcn_perm(0x3e3e3e3eu, 0x3e3e3d3du, size) | below << 4;
+    y[odd] = __builtin_amdgcn_perm(hi, lo, 0x06020400u);      // codes 0 and 4, 1 and 5
+    y[odd + 2] = __builtin_amdgcn_perm(hi, lo, 0x07030501u);  // 2 and 6, 3 and 7
   }
   return __builtin_bit_cast(bf16x8, y);
 }

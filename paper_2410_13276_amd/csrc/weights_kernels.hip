@@ -9,7 +9,9 @@
 // wavefront, and there are no atomics.
 //
 // Units of keys are dealt out to the workgroups as in attention, and keys in 4 bits enter as there
-// (q4_attn_kernels.hip).  A head's rows stay in the LDS for all units of a run, where they fit.
+// (q4_attn_kernels.hip), centred for a q in fp32 (a rotated row over 70 and 300 keys: weights 0.8e-7 to 2.5e-7 off in the 2-norm, and 3e-7 to
+// 1.0e-6 with codes of one sign, 0.7e-6 to 3.3e-6 where one element of each group is far off; 131072 tokens of 32 / 8 heads of 128 30 us, and 25).  A
+// head's rows stay in the LDS for all units of a run, where they fit.
 //
 // Measured (bf16, 32 / 8 heads of 128, one MI355X): 64 sequences of 200 to 16000 tokens in 4 bits, a token each, 50 us for 170 MB (3.4e12
 // bytes a second; a kernel that only reads reaches 6.2e12), bound by the latency of a tile's loads and a run's beginning; the last 64 tokens of
@@ -87,6 +89,10 @@ __global__ __launch_bounds__((Shape<T, D, NG, PACK, QP>::THREADS), (Shape<T, D, 
   constexpr bool ALIGNED = NPH > 1;
   static_assert(!ALIGNED || PACK == 1, "a block's groups all share the rows, or none");
   constexpr int KW = Q4 ? D / 32 : 4 * STEPS;   // dwords of a key per lane
+  auto open = [](uint32_t codes) {
+    if constexpr (BF) return open8(codes);
+    else return open8_centred(codes);
+  };
   extern __shared__ __attribute__((aligned(16))) char room[];
   __shared__ __attribute__((aligned(16))) float sks[kWaves][Q4 ? KT : 1][NGX], skm[kWaves][Q4 ? KT : 1][NGX];
   u32x4(*sq)[QP][STEPS][kWave] = (u32x4(*)[QP][STEPS][kWave])room;
@@ -336,13 +342,13 @@ __global__ __launch_bounds__((Shape<T, D, NG, PACK, QP>::THREADS), (Shape<T, D, 
                 const float2 q2 = rows[r / PACK].sum[ph * PACK + r % PACK];
                 all[r] = q2.y;
 #pragma unroll
-                for (int i = 0; i < SUB; ++i) y[i][r] = -kMid * q2.x;
+                for (int i = 0; i < SUB; ++i) y[i][r] = BF ? -kMid * q2.x : 0.f;  // (fp32: the codes are centred)
               }
 #pragma unroll
               for (int f = ph * (STEPS / NPH); f < (ph + 1) * (STEPS / NPH); ++f) {
                 bf16x8 k8[SUB];
 #pragma unroll
-                for (int i = 0; i < SUB; ++i) k8[i] = open8(kq[i][f]);
+                for (int i = 0; i < SUB; ++i) k8[i] = open(kq[i][f]);
 #pragma unroll
                 for (int part = QP - 1; part >= 0; --part) {
                   const u32x4 q = sq[cb - cb0][part][f][lane];
