@@ -69,6 +69,7 @@ struct Shape {
   // of a block: the operand as the lanes read it, rows, cosines and sines of their tokens
   static constexpr int OPERAND = QP * STEPS * kWave * 16;
   static constexpr int BYTES = OPERAND + ROWS * (int)sizeof(Row) + (TURNS ? ROWS * (D / 2) * 8 : 0);
+  static constexpr int MOST = kRoom > BYTES ? kRoom / BYTES : 1;  // blocks that the LDS holds
   // per SIMD, as the registers allow (4 bits of 128 elements with q in three parts: 4 spill 26, and a token after 131072 takes 39.5
   // us for 27.1)
   static constexpr int WAVES = !Q4 || NG == 1 ? 4 : PACK == 1 ? 2 : D == 128 && QP == 3 ? 3 : 4;
@@ -474,7 +475,7 @@ hipError_t launch(KernelArgs& k, hipStream_t s) {
   auto units = [&]() -> int64_t { return ((int64_t)k.capacity + ((int64_t)1 << k.unit_shift) - 1) >> k.unit_shift; };
   while ((units() + 1) * heads > (1 << 30)) ++k.unit_shift;
   k.blocks = (k.rows + S::ROWS - 1) / S::ROWS;
-  k.held = std::min(k.blocks, std::max(1, kRoom / S::BYTES));
+  k.held = std::min(k.blocks, S::MOST);
   // as many workgroups as the GPU holds at once: by registers, and by the LDS
   const int lds = k.held * S::BYTES + (S::Q4 ? kWaves * S::KT * NG * 8 : 0);
   const int per_cu = std::max(1, std::min(S::WAVES * 4 / kWaves, (160 << 10) / (lds + 1024)));
@@ -486,7 +487,8 @@ hipError_t launch(KernelArgs& k, hipStream_t s) {
   auto kernel = k.a.q.cache.table.page.d % 16 == 0 && k.kss < far ? weights_kernel<T, D, NG, PACK, QP, true>
                                                                  : weights_kernel<T, D, NG, PACK, QP, false>;
   if (lds > 64 << 10) {
-    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)room);
+    // (the kernel's, not the call's: every call sets the same, as others may be between theirs and their launch)
+    const hipError_t e = hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::MOST * S::BYTES);
     if (e != hipSuccess) return e;
   }
   kernel<<<grid, S::THREADS, room, s>>>(k);
