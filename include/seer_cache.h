@@ -172,7 +172,7 @@ size_t seer_kv_evict_workspace_bytes(const seer_kv_cache* cache, int32_t batch);
  * holds, nor stand in it twice, and weights may not overlap new_weights.  A kept slot whose page is none is not moved.  Every other slot is left as it
  * is.  workspace: device memory of seer_kv_evict_workspace_bytes, 256-byte aligned, not shared with a call that may run at
  * the same time; its contents need no set-up.  NULL where that is 0.
- * SEER_ERR_UNSUPPORTED: as seer_kv_append, more than 65535 KV heads or 2^22 pairs of sequence and head.
+ * SEER_ERR_UNSUPPORTED: as seer_kv_append, more than 65535 KV heads, 2^22 pairs of sequence and head and more.
  */
 seer_status seer_kv_evict(const seer_kv_cache* cache, const seer_kv_eviction* desc, void* workspace, size_t workspace_bytes,
                           void* stream);

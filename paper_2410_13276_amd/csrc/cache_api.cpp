@@ -6,7 +6,7 @@
 
 namespace {
 
-constexpr int64_t kMostPairs = (int64_t)1 << 22;  // of sequence and KV head, of one eviction
+constexpr int64_t kMostPairs = ((int64_t)1 << 22) - 1;  // of sequence and KV head, of one eviction (workgroups of 1024, less than 2^32 threads)
 constexpr float kMostScale = 0x1p100f;            // (16 log2(e) times it is finite, which the weights' arguments need)
 
 // One pool's pointers and strides.
