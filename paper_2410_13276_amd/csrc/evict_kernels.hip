@@ -8,9 +8,12 @@
 // the histograms too.  A last launch moves the keys and values, 16 bytes a thread, whatever they are held as: the places it
 // writes are no places that it reads, so that it needs no order.
 //
-// Measured, one MI355X: 64 sequences of 1700 to 2400 slots cut to 2048 (8 heads of 128 in 4 bits) 15 us to choose, 57 to move 336 MB at
-// 5.9e12 bytes a second, the memory's rate; 131072 slots cut to 4096 (bf16) 41 us to choose, by launches and barriers (the weights are 4 MB), 7.5 to move 34 MB.
-// A row of 131072 slots by one workgroup a head takes 185 us to choose.
+// Measured, one MI355X: 64 sequences of 1700 to 2400 slots cut to 2048 (8 heads of 128 in 4 bits) 15 us to choose, 57 to move 336
+// MB at 5.9e12 bytes a second, the memory's rate; 131072 slots cut to 4096 (bf16) 41 us to choose, by launches and barriers (the
+// weights are 4 MB; the digits' launches take 5.9, 9.8 and 9.8 us, the one that writes 15.6; equal addresses of the LDS, nearly all
+// in the first, cost it 1.0e5 cycles over 64 workgroups, 0.7 us), 7.7 to move 34 MB. A row of 131072 slots by one workgroup a head
+// takes 185 us to choose; what has more than 128 pairs is done so (64 sequences of 8 heads of 131072 slots cut to 1024: 389 us
+// together, whose bytes take 164).
 #include <algorithm>
 
 #include "cache.h"
@@ -292,7 +295,9 @@ struct MoveArgs {
 
 // LANES threads move an entry, each 16 bytes of its key and of its value; PARAMS: and a dword of their params.  (There are more
 // threads than sequences.)
-// PAST: past the caches, which pays where more is moved than they hold (168 MB of 4 bits 70.7 -> 57.6 us, 17 MB of bf16 7.7 -> 9.1).
+// PAST: past the caches, from 64 MiB on (8 heads of 128 in 4 bits, pages that no cache holds, selection included: 134 MB 87 -> 78
+// us, 268 MB 168 -> 152; bf16 134 MB 62 -> 57, 268 MB 112 -> 101; 34 MB 23.8 -> 23.3, of 4 bits 30.5 -> 28.4).  What the caches may
+// hold yet takes longer past them (17 MB of bf16 7.7 -> 9.1, a whole call of 67 MB 26 -> 31).
 template <int LANES, int PARAMS, bool PAST>
 __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs ka) {
   const EvictArgs& a = ka.a;
@@ -336,7 +341,10 @@ __global__ __launch_bounds__(256) void evict_move_kernel(MoveArgs ka) {
   }
 }
 
-// Parts of a row: as many as give the GPU work, of kPart slots or more.
+// Parts of a row: as many as give the GPU work, of kPart slots or more.  256 workgroups: 128 rows of 131072 slots cut to 1024 take
+// 165 us whole, 126 in 2 parts, 123 in 4; 256 rows 207 whole, 220 in 2 parts.  At most 32 parts: two rows of 1048576 slots 92 us in
+// 16, 75 in 32, 81 in 64.  (The table's room counts, as the lengths are on the device: 3000 slots in a table of 131072 take 26 us,
+// of 4096 14.)
 int parts_of(int64_t pairs, int capacity) {
   return (int)std::max((int64_t)1, std::min({((int64_t)capacity + kPart - 1) / kPart, 256 / pairs, (int64_t)32}));
 }

@@ -1,7 +1,7 @@
 // q4_attn_kernels.hip -- attention of new tokens over a paged cache held in 4 bits.
 //
 // As over a cache of values (paged_attn_kernels.hip) the rows of a KV group are the columns of S^T = K Q^T and O^T = V^T P^T, and
-// the units of all sequences' keys are dealt out evenly to the workgroups.  What differs is that a key is 40 to 80 bytes and
+// the units of all sequences' keys are dealt out evenly to the workgroups.  What differs is that a key is 36 to 80 bytes and
 // has to be opened: at 5 bits an element HBM brings about 8e12 elements a second, for which the
 // vector units have some 4 operations each.  So codes enter the matrix products as they are, and steps and
 // middles are applied to what comes out or goes in:
@@ -34,11 +34,12 @@
 // fp32; where it is bf16, in two, 2^-18 of it off at most, where the output's own rounding is 2^-9.
 //
 // Measured (bf16, one MI355X): 32 / 8 heads of 128 in groups of 32, a token after 131072 tokens 42 us + 4 of the join, for 168 MB
-// (4e12 bytes a second while it runs; a kernel that only reads reaches 6.2e12); 64 sequences of 200 to 16000 tokens 77 + 4.5 for 285
-// MB.  What bounds it is latency: a wavefront has one tile, 10 KB, in flight, two a SIMD, and its registers are used up (a second
-// tile spills: 79 us); the vector units issue 0.46 of the time, the matrix units work 0.2.  About 9 us are a run's beginning (positions, table,
-// tile, one after the other) and end.  With 16 rows and more a tile's own chain is what takes long, scores, weights and factors of two or
-// four phases: 28 rows of 4 heads over 93643 tokens in groups of 64 46 us for 54 MB.
+// (4e12 bytes a second while it runs; a kernel that only reads reaches 6.2e12); 64 sequences of 200 to 16000 tokens 77 + 4.5 for
+// 285 MB.  What bounds it is latency, a tile's chain of dependent steps at two wavefronts a SIMD first (without any loads it takes
+// 34 us of 43, without products 39), its loads beside it (one tile, 10 KB, in flight a wavefront; a second in registers spills: 79
+// us); the vector units issue 0.46 of the time, the matrix units work 0.2.  About 9 us are a run's beginning (positions, table,
+// tile, one after the other) and end.  With 16 rows and more a tile's own chain is what takes long, scores, weights and factors of
+// two or four phases: 28 rows of 4 heads over 93643 tokens in groups of 64 46 us for 54 MB.
 #include <algorithm>
 #include <type_traits>
 
@@ -106,9 +107,8 @@ __device__ __forceinline__ float row_sum(float x) {
 
 // D: elements of a head.  NG: groups of a head.  PACK: of them, those that share the columns.  QP: bf16 parts of q (1: bf16
 // as it is, 3: rotated, or fp32).
-// RUN: pages hold whole aligned runs of 16
-// keys, whose rows lie within 2^30 bytes (a token after 131072 tokens: 50 us a call, pages of 64 and of 24, which
-// are looked up key by key, alike; pages of 1 82).
+// RUN: pages hold whole aligned runs of 16 keys, whose rows lie within 2^30 bytes (a token after 131072 tokens, replayed from a
+// graph: pages of 64 46 us, of 24, which are looked up key by key, 50, of 1 81).
 template <typename T, int D, int NG, int PACK, int QP, bool RUN>
 __global__ __launch_bounds__(kThreads, 2) void q4_attn_kernel(KernelArgs ka) {
   constexpr int ROWS = 16 / PACK, NPH = NG / PACK;

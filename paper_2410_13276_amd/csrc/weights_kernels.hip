@@ -13,10 +13,10 @@
 // 1.0e-6 with codes of one sign, 0.7e-6 to 3.3e-6 where one element of each group is far off; 131072 tokens of 32 / 8 heads of 128 30 us, and 25).  A
 // head's rows stay in the LDS for all units of a run, where they fit.
 //
-// Measured (bf16, 32 / 8 heads of 128, one MI355X): 64 sequences of 200 to 16000 tokens in 4 bits, a token each, 50 us for 170 MB (3.4e12
-// bytes a second; a kernel that only reads reaches 6.2e12), bound by the latency of a tile's loads and a run's beginning; the last 64 tokens of
-// 32768 over bf16 keys, 41 us for 68 MB: 256 rows, whose exponentials, products and sums take half of the units' time; the rest is waits for the rows' operands and
-// factors out of the LDS.
+// Measured (bf16, 32 / 8 heads of 128, one MI355X): 64 sequences of 200 to 16000 tokens in 4 bits, a token each, 49 us for 170 MB
+// (3.4e12 bytes a second; a kernel that only reads reaches 6.2e12), bound by the latency of a tile's loads and a run's beginning;
+// the last 64 tokens of 32768 over bf16 keys, 43 us for 68 MB: 256 rows, whose exponentials, products and sums take half of the
+// units' time; the rest is waits for the rows' operands and factors out of the LDS.
 #include <algorithm>
 
 #include "cache.h"
