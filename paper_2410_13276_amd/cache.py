@@ -262,7 +262,8 @@ def paged_attn_q4(q, k_cache, v_cache, table, positions, *, inv_freq=None, rope_
                   workspace=None, stream=None):
     """Attention of new tokens over a paged cache held in 4 bits (seer_paged_attn_q4).  Arguments and results as
     paged_attn's, the caches Q4Pools, positions the last slot that each token sees; inv_freq: q is rotated first, at
-    rope_positions (None: positions).  Returns (O, LSE [B, Hq, S] ([B, Hq]) or None)."""
+    rope_positions (None: positions).  The keys are opened again for every 16 rows (query heads of a KV head times tokens): with more rows than
+    that the call is no faster than paged_attn over bf16.  Returns (O, LSE [B, Hq, S] ([B, Hq]) or None)."""
     if _d._t is None:
         _d._load()
     (batch, heads, tokens, dim), qs = _d._tokens_of(q, "q")
@@ -366,7 +367,8 @@ def kv_evict(k_cache, v_cache, table, lengths, weights, new_table, keep: int, *,
     [B], slots in use; weights: float32 [B, Hkv, W].  The pages of new_table may not be ones that the table's rows hold.
     out: (lengths int32 [B], which may be `lengths`, kept int32 [B, Hkv, keep], weights float32 [B, Hkv, W' >= keep]) to write to, the latter with 0
     behind the kept slots' weights; None: new ones, W' what new_table has room for.  Returns them; kept says which slots
-    they were (-1 where a sequence had fewer)."""
+    they were (-1 where a sequence had fewer).  A table with room for many more slots than the sequences hold (16384 and more of few
+    heads) costs three more launches, 12 us: table[:, :n] avoids them."""
     if _d._t is None:
         _d._load()
     dev = lengths.get_device()
